@@ -343,6 +343,100 @@ int he_round_host(he_ctx *ctx, const he_keys *keys, const he_mask *mask, const f
                   const double *alpha_host, int C, size_t P, uint64_t enc_seed, double *w_glob_host,
                   void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Sensitivity(W, D_i) of Algorithm 1 ("Step 1" of Selective Parameter
+ * Encryption): the scores that he_select_mask takes,
+ *   S_m = 1/K sum_k | d/dy_k (d loss / dw_m) |.
+ * Under cross entropy loss_k = -sum_c y_{k,c} log p_c the derivative by the
+ * coordinate of the sample's label is, up to its sign, d log p_{y_k} / dw_m;
+ * a sequence's is that of the sum over its tokens.  The operators below are
+ * what a client needs for the map of a language model beside products that it
+ * has: log probabilities and their gradient (where the backward pass begins),
+ * layer norm, and, for layer norm and linear layers, the sums over samples of
+ * magnitudes of gradients, of which none is ever in memory by itself.
+ *
+ * Common to them:
+ *   - dtype is HE_F32, HE_BF16 or HE_F16; matrices are row-major with a row
+ *     stride in elements (0 repeats a row of an input; an output's is at least
+ *     its width) and need only their elements' alignment.  Rows that begin on
+ *     16-byte boundaries are faster.
+ *   - Samples are runs of rows that follow one another: sample k has the rows
+ *     [samples[k], samples[k+1]), samples: dev int32 [num_samples + 1],
+ *     ascending.  Empty samples add nothing, and rows before the first or
+ *     behind the last (a batch's padding) belong to none.  Offsets that are not
+ *     ascending or reach beyond the rows give unspecified sums, never an access
+ *     out of bounds.
+ *   - Statistics, sums and map entries are fp32 whatever the dtype.  Results
+ *     do not depend on timing: the same call gives the same bits.
+ *   - Nothing is allocated: scratch comes from the caller (work, 16-byte
+ *     aligned, of at least the bytes that *_work_bytes names), so calls that
+ *     have scratch of their own may overlap on any streams, and all of
+ *     them can be captured.  The context's GPU must be the current device
+ *     (HE_ERR_INVALID_ARG).
+ *   - rows < 2^28 and columns < 2^31 (HE_ERR_SIZE).
+ * ------------------------------------------------------------------------- */
+enum { HE_F32 = 0, HE_BF16 = 1, HE_F16 = 2 };
+#define HE_MAX_TOP 64
+
+/* For every row z of logits (dev [rows][vocab]):
+ *   lse = ln sum_j e^(z_j),   entropy = -sum_j p_j ln p_j,   p = e^(z - lse),
+ *   logp = z_y - lse for the row's target y; 0 where y < 0 (no target), NaN
+ *   where y >= vocab,
+ *   top_logp, top_ids [rows][top]: the `top` highest log probabilities, equal
+ *   ones by the lowest index; top <= HE_MAX_TOP and <= vocab; 0: none, and the
+ *   pointers may be NULL.
+ * Logits of -inf (a vocabulary's mask) have p = 0.  In a row of nothing but
+ * -inf lse, logp and top_logp are -inf and the entropy is 0.  A NaN or +inf
+ * makes the row's numbers NaN; NaN ranks with -inf among the alternatives.
+ * targets: dev int64 [rows]; logp, lse, entropy: dev float [rows]. */
+int he_token_log_probs(he_ctx *ctx, const void *logits_dev, int dtype, size_t rows, size_t vocab, size_t row_stride,
+                       const int64_t *targets_dev, uint32_t top, float *logp_dev, float *lse_dev, float *entropy_dev,
+                       float *top_logp_dev, int64_t *top_ids_dev, void *stream);
+/* Its gradient, from the lse (and entropy) that it gave:
+ *   dlogits_j = sum_i g_i (d_{j,t_i} - p_j) - dentropy p_j (ln p_j + entropy)
+ * over the target (g = dlogp; none for y < 0) and the alternatives (t =
+ * top_ids, g = dtop, [rows][top]; top = 0: none).  dentropy may be NULL, and
+ * entropy then too.  A row into which no gradient flows (no target, no
+ * dentropy, no dtop) or that holds nothing but -inf gives zeros whatever it
+ * holds.  dlogits may be logits itself, with the same stride. */
+int he_token_log_probs_backward(he_ctx *ctx, const void *logits_dev, int dtype, size_t rows, size_t vocab, size_t row_stride,
+                                const int64_t *targets_dev, const float *lse_dev, const float *dlogp_dev,
+                                const float *entropy_dev, const float *dentropy_dev, uint32_t top,
+                                const int64_t *top_ids_dev, const float *dtop_dev, void *dlogits_dev,
+                                size_t dlogits_stride, void *stream);
+
+/* Layer norm of the rows of x:  y = (x - mean) rstd weight + bias,
+ * rstd = 1 / sqrt(mean((x - mean)^2) + eps).  weight and bias [width] are of
+ * weight_dtype and may be NULL (1 and 0); mean, rstd: dev float [rows], for the
+ * backward pass.  y has x's dtype and may be x itself, with the same stride. */
+int he_layer_norm(he_ctx *ctx, const void *x_dev, int dtype, size_t rows, size_t width, size_t x_stride,
+                  const void *weight_dev, const void *bias_dev, int weight_dtype, float eps, void *y_dev,
+                  size_t y_stride, float *mean_dev, float *rstd_dev, void *stream);
+/* Its backward pass.  dx is the gradient of x (of x's dtype, every row; not x
+ * or dy itself).  samples_dev == NULL: dweight = sum_t dy_t n_t, dbias = sum_t
+ * dy_t over all rows, n = (x - mean) rstd.  Otherwise the map's entries:
+ * sum_k |sum_{t in k} dy_t n_t| and sum_k |sum_{t in k} dy_t|.
+ * dweight, dbias: dev float [width], overwritten. */
+size_t he_layer_norm_backward_work_bytes(const he_ctx *ctx, size_t rows, size_t width);
+int he_layer_norm_backward(he_ctx *ctx, const void *dy_dev, size_t dy_stride, const void *x_dev, size_t x_stride, int dtype,
+                           size_t rows, size_t width, const float *mean_dev, const float *rstd_dev,
+                           const void *weight_dev, int weight_dtype, const int32_t *samples_dev, size_t num_samples,
+                           void *dx_dev, size_t dx_stride, float *dweight_dev, float *dbias_dev, void *work_dev,
+                           size_t work_bytes, void *stream);
+
+/* Map entries of a linear layer y = x W^T + b from its inputs x [rows][inputs]
+ * and the gradients dy [rows][outputs] of its outputs:
+ *   weight[o][i] = sum_k |sum_{t in k} dy[t][o] x[t][i]|,
+ *   bias[o]      = sum_k |sum_{t in k} dy[t][o]|.
+ * samples_dev == NULL: every row is a sample of its own.  weight: dev float
+ * [outputs][inputs], bias: dev float [outputs] or NULL; overwritten, or added
+ * to if accumulate is not 0. */
+size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs);
+int he_linear_sensitivity(he_ctx *ctx, const void *x_dev, size_t x_stride, const void *dy_dev, size_t dy_stride, int dtype,
+                          size_t rows, size_t inputs, size_t outputs, const int32_t *samples_dev, size_t num_samples,
+                          int accumulate, float *weight_dev, float *bias_dev, void *work_dev, size_t work_bytes,
+                          void *stream);
+
 /* Number of kernel launches issued by this library since it was loaded. */
 uint64_t he_launch_count(void);
 

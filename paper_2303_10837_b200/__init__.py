@@ -87,6 +87,14 @@ _SIGS = {
     "he_ntt_forward": (C.c_int, [_vp, _vp, _sz, _vp]),
     "he_ntt_inverse": (C.c_int, [_vp, _vp, _sz, _vp]),
     "he_round_host": (C.c_int, [_vp, _vp, _vp, _vp, _vp, C.c_int, _sz, _u64, _vp, _vp]),
+    "he_token_log_probs": (C.c_int, [_vp, _vp, C.c_int, _sz, _sz, _sz, _vp, _u32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "he_token_log_probs_backward": (C.c_int, [_vp, _vp, C.c_int, _sz, _sz, _sz, _vp, _vp, _vp, _vp, _vp, _u32, _vp, _vp, _vp, _sz, _vp]),
+    "he_layer_norm": (C.c_int, [_vp, _vp, C.c_int, _sz, _sz, _sz, _vp, _vp, C.c_int, C.c_float, _vp, _sz, _vp, _vp, _vp]),
+    "he_layer_norm_backward_work_bytes": (_sz, [_vp, _sz, _sz]),
+    "he_layer_norm_backward": (C.c_int, [_vp, _vp, _sz, _vp, _sz, C.c_int, _sz, _sz, _vp, _vp, _vp, C.c_int, _vp, _sz, _vp, _sz, _vp, _vp,
+                                         _vp, _sz, _vp]),
+    "he_linear_sensitivity_work_bytes": (_sz, [_vp, C.c_int, _sz, _sz, _sz]),
+    "he_linear_sensitivity": (C.c_int, [_vp, _vp, _sz, _vp, _sz, C.c_int, _sz, _sz, _sz, _vp, _sz, C.c_int, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -546,3 +554,213 @@ def he_round_host(ctx: Ctx, keys: Keys, mask: Optional[Mask], xs: List[torch.Ten
     _check(_lib.he_round_host(ctx.handle, keys.handle, mask.handle if mask else None, C.cast(ptrs, _vp),
                               C.cast(al, _vp), Cn, P, enc_seed, out.data_ptr(), _stream()), "he_round_host")
     return out
+
+
+# ---------------------------------------------------------------------------
+# the sensitivity map's operators (Step 1 of Selective Parameter Encryption)
+# ---------------------------------------------------------------------------
+
+HE_F32, HE_BF16, HE_F16 = 0, 1, 2
+HE_MAX_TOP = 64
+_DTYPES = {torch.float32: HE_F32, torch.bfloat16: HE_BF16, torch.float16: HE_F16}
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise HeError(HE_ERR_INVALID_ARG, "%s: %s, not float32, bfloat16 or float16" % (what, t.dtype))
+    return code
+
+
+def _matrix(t: torch.Tensor, rows: Optional[int], cols: Optional[int], dtype: Optional[torch.dtype], what: str, out: bool = False) -> int:
+    """Row stride of a matrix whose rows are contiguous; its sizes and type are checked (None: any)."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise HeError(HE_ERR_INVALID_ARG, "%s: shape %s, [%s][%s] needed" % (what, tuple(t.shape), "rows" if rows is None else rows,
+                                                                             "columns" if cols is None else cols))
+    if dtype is not None and t.dtype != dtype:
+        raise HeError(HE_ERR_INVALID_ARG, "%s: %s, %s needed" % (what, t.dtype, dtype))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise HeError(HE_ERR_INVALID_ARG, "%s: the elements of a row do not lie together" % what)
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if out and stride < t.shape[1]:
+        raise HeError(HE_ERR_INVALID_ARG, "%s: rows overlap" % what)
+    return stride
+
+
+def _vector(t: torch.Tensor, count: int, dtype, what: str) -> None:
+    if t.dim() != 1 or t.shape[0] != count or t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)) or (count > 1 and t.stride(0) != 1):
+        raise HeError(HE_ERR_INVALID_ARG, "%s: %s %s, a contiguous vector of %d needed" % (what, t.dtype, tuple(t.shape), count))
+
+
+def _on_gpu(first: torch.Tensor, *more: Optional[torch.Tensor]) -> int:
+    """All tensors lie on the current device (None: absent)."""
+    device = torch.cuda.current_device() if first.is_cuda else -1
+    for t in (first,) + more:
+        if t is not None:
+            if not t.is_cuda:
+                raise TypeError("expected CUDA tensors")
+            if t.get_device() != device:
+                raise HeError(HE_ERR_INVALID_ARG, "a tensor on cuda:%d, the current device is cuda:%d" % (t.get_device(), device))
+    return device
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr() or None
+
+
+def _offsets(samples: Optional[torch.Tensor], what: str) -> int:
+    """Number of samples of a vector of offsets."""
+    if samples is None:
+        return 0
+    if samples.dim() != 1 or samples.shape[0] < 1 or samples.dtype != torch.int32 or not samples.is_contiguous():
+        raise HeError(HE_ERR_INVALID_ARG, "%s: %s %s, contiguous int32 offsets needed" % (what, samples.dtype, tuple(samples.shape)))
+    return samples.shape[0] - 1
+
+
+def he_token_log_probs(ctx: Ctx, logits: torch.Tensor, targets: torch.Tensor, top: int = 0):
+    """(logp, lse, entropy: float32 [rows]; top_logp float32, top_ids int64: [rows][top], None for top = 0) of logits [rows][vocab]
+    and int64 targets, of which a negative one is none."""
+    what = "he_token_log_probs "
+    code, stride = _dtype(logits, what + "logits"), _matrix(logits, None, None, None, what + "logits")
+    rows, vocab = logits.shape
+    _vector(targets, rows, torch.int64, what + "targets")
+    if vocab < 1 or not 0 <= top <= min(vocab, HE_MAX_TOP):
+        raise HeError(HE_ERR_INVALID_ARG, what + "top: %d of %d" % (top, vocab))
+    _on_gpu(logits, targets)
+    out = torch.empty((3, rows), dtype=torch.float32, device=logits.device)
+    logp, lse, entropy = out.unbind(0)
+    top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device) if top else None
+    top_ids = torch.empty((rows, top), dtype=torch.int64, device=logits.device) if top else None
+    _check(_lib.he_token_log_probs(ctx.handle, _ptr(logits), code, rows, vocab, stride, _ptr(targets), top, _ptr(logp), _ptr(lse),
+                                   _ptr(entropy), _ptr(top_logp), _ptr(top_ids), _stream()), "he_token_log_probs")
+    return logp, lse, entropy, top_logp, top_ids
+
+
+def he_token_log_probs_backward(ctx: Ctx, logits: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor,
+                                entropy: Optional[torch.Tensor] = None, dentropy: Optional[torch.Tensor] = None,
+                                top_ids: Optional[torch.Tensor] = None, dtop: Optional[torch.Tensor] = None,
+                                out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of the logits, of their type, from those of logp and, where given, of the entropy and of the alternatives; `out` may
+    be the logits themselves."""
+    what = "he_token_log_probs_backward "
+    code, stride = _dtype(logits, what + "logits"), _matrix(logits, None, None, None, what + "logits")
+    rows, vocab = logits.shape
+    _vector(targets, rows, torch.int64, what + "targets")
+    _vector(lse, rows, torch.float32, what + "lse")
+    _vector(dlogp, rows, torch.float32, what + "dlogp")
+    if dentropy is not None:
+        if entropy is None:
+            raise HeError(HE_ERR_INVALID_ARG, what + "dentropy needs the entropy")
+        _vector(entropy, rows, torch.float32, what + "entropy")
+        _vector(dentropy, rows, torch.float32, what + "dentropy")
+    top = 0
+    if (top_ids is None) != (dtop is None):
+        raise HeError(HE_ERR_INVALID_ARG, what + "top_ids and dtop go together")
+    if top_ids is not None:
+        top = top_ids.shape[1] if top_ids.dim() == 2 else -1
+        if not 0 <= top <= min(vocab, HE_MAX_TOP) or top_ids.shape != (rows, top) or dtop.shape != (rows, top) or top_ids.dtype != torch.int64 or \
+                dtop.dtype != torch.float32 or not top_ids.is_contiguous() or not dtop.is_contiguous():
+            raise HeError(HE_ERR_INVALID_ARG, what + "top_ids %s and dtop %s" % (tuple(top_ids.shape), tuple(dtop.shape)))
+    if vocab < 1:
+        raise HeError(HE_ERR_INVALID_ARG, what + "logits: no columns")
+    if out is not None:
+        _matrix(out, rows, vocab, logits.dtype, what + "out", out=True)
+    _on_gpu(logits, targets, lse, dlogp, entropy, dentropy, top_ids, dtop, out)
+    if out is None:
+        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+    _check(_lib.he_token_log_probs_backward(ctx.handle, _ptr(logits), code, rows, vocab, stride, _ptr(targets), _ptr(lse), _ptr(dlogp),
+                                            _ptr(entropy) if dentropy is not None else None, _ptr(dentropy), top, _ptr(top_ids) if top else None,
+                                            _ptr(dtop) if top else None, _ptr(out), out.stride(0) if rows > 1 else vocab, _stream()),
+           "he_token_log_probs_backward")
+    return out
+
+
+def _norm_weights(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], width: int, x: torch.Tensor, what: str) -> int:
+    """Type of the weights: float32 or x's, both the same."""
+    kinds = [t.dtype for t in (weight, bias) if t is not None]
+    for t in (weight, bias):
+        if t is not None:
+            _vector(t, width, (torch.float32, x.dtype), what + "weights")
+    if len(kinds) == 2 and kinds[0] != kinds[1]:
+        raise HeError(HE_ERR_INVALID_ARG, what + "weight and bias: %s and %s" % (kinds[0], kinds[1]))
+    return _DTYPES[kinds[0]] if kinds else HE_F32
+
+
+def he_layer_norm(ctx: Ctx, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                  out: Optional[torch.Tensor] = None):
+    """(y of x's type, mean, rstd: float32 [rows]) of the rows of x; `out` may be x itself."""
+    what = "he_layer_norm "
+    code, stride = _dtype(x, what + "x"), _matrix(x, None, None, None, what + "x")
+    rows, width = x.shape
+    kind = _norm_weights(weight, bias, width, x, what)
+    if width < 1 or not eps >= 0:
+        raise HeError(HE_ERR_INVALID_ARG, what + "width %d, eps %g" % (width, eps))
+    if out is not None:
+        _matrix(out, rows, width, x.dtype, what + "out", out=True)
+    _on_gpu(x, weight, bias, out)
+    if out is None:
+        out = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    _check(_lib.he_layer_norm(ctx.handle, _ptr(x), code, rows, width, stride, _ptr(weight), _ptr(bias), kind, eps, _ptr(out),
+                              out.stride(0) if rows > 1 else width, _ptr(mean), _ptr(rstd), _stream()), "he_layer_norm")
+    return out, mean, rstd
+
+
+def he_layer_norm_backward(ctx: Ctx, dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                           weight: Optional[torch.Tensor] = None, samples: Optional[torch.Tensor] = None):
+    """(dx of x's type, dweight, dbias: float32 [width]).  With the offsets of samples the last two are the map's entries, sums over
+    samples of magnitudes; without, gradients over all rows."""
+    what = "he_layer_norm_backward "
+    code, stride = _dtype(x, what + "x"), _matrix(x, None, None, None, what + "x")
+    rows, width = x.shape
+    dy_stride = _matrix(dy, rows, width, x.dtype, what + "dy")
+    _vector(mean, rows, torch.float32, what + "mean")
+    _vector(rstd, rows, torch.float32, what + "rstd")
+    kind = _norm_weights(weight, None, width, x, what)
+    count = _offsets(samples, what + "samples")
+    if width < 1:
+        raise HeError(HE_ERR_INVALID_ARG, what + "x: no columns")
+    _on_gpu(x, dy, mean, rstd, weight, samples)
+    dx = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+    dweight, dbias = torch.empty((2, width), dtype=torch.float32, device=x.device).unbind(0)
+    room = _lib.he_layer_norm_backward_work_bytes(ctx.handle, rows, width)
+    work = torch.empty(max(room, 16), dtype=torch.uint8, device=x.device)
+    _check(_lib.he_layer_norm_backward(ctx.handle, _ptr(dy), dy_stride, _ptr(x), stride, code, rows, width, _ptr(mean), _ptr(rstd), _ptr(weight),
+                                       kind, _ptr(samples), count, _ptr(dx), width, _ptr(dweight), _ptr(dbias), _ptr(work), work.numel(),
+                                       _stream()), "he_layer_norm_backward")
+    return dx, dweight, dbias
+
+
+def he_linear_sensitivity(ctx: Ctx, x: torch.Tensor, dy: torch.Tensor, samples: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None, out_bias: Optional[torch.Tensor] = None, accumulate: bool = False,
+                          bias: bool = True):
+    """(float32 [outputs][inputs], float32 [outputs] or None without bias): a linear layer's entries of the map from its inputs
+    x [rows][inputs] and its outputs' gradients dy [rows][outputs], summed over samples, or over rows without offsets; with `accumulate`
+    added to what out and out_bias hold."""
+    what = "he_linear_sensitivity "
+    code, stride = _dtype(x, what + "x"), _matrix(x, None, None, None, what + "x")
+    rows, inputs = x.shape
+    dy_stride = _matrix(dy, rows, None, x.dtype, what + "dy")
+    outputs = dy.shape[1]
+    count = _offsets(samples, what + "samples")
+    if inputs < 1 or outputs < 1:
+        raise HeError(HE_ERR_INVALID_ARG, what + "%d inputs, %d outputs" % (inputs, outputs))
+    if accumulate and (out is None or (bias and out_bias is None)):
+        raise HeError(HE_ERR_INVALID_ARG, what + "nothing to add to")
+    if out is not None:
+        _matrix(out, outputs, inputs, torch.float32, what + "out", out=True)
+        if not out.is_contiguous():
+            raise HeError(HE_ERR_INVALID_ARG, what + "out is not contiguous")
+    if out_bias is not None:
+        _vector(out_bias, outputs, torch.float32, what + "out_bias")
+    _on_gpu(x, dy, samples, out, out_bias)
+    if out is None:
+        out = torch.empty((outputs, inputs), dtype=torch.float32, device=x.device)
+    if bias and out_bias is None:
+        out_bias = torch.empty(outputs, dtype=torch.float32, device=x.device)
+    room = _lib.he_linear_sensitivity_work_bytes(ctx.handle, code, rows, inputs, outputs)
+    work = torch.empty(max(room, 16), dtype=torch.uint8, device=x.device)
+    _check(_lib.he_linear_sensitivity(ctx.handle, _ptr(x), stride, _ptr(dy), dy_stride, code, rows, inputs, outputs, _ptr(samples), count,
+                                      1 if accumulate else 0, _ptr(out), _ptr(out_bias) if bias else None, _ptr(work), work.numel(), _stream()),
+           "he_linear_sensitivity")
+    return out, out_bias if bias else None

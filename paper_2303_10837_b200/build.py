@@ -18,10 +18,10 @@ OUT = os.path.join(HERE, "libfedhe.so")
 BUILD = os.path.join(HERE, "_build")
 
 CUDA_SOURCES = ["fedhe_transform.cu", "fedhe_slots.cu", "fedhe_encrypt.cu", "fedhe_fft.cu", "fedhe_server.cu", "fedhe_decrypt.cu",
-                "fedhe_mask.cu", "fedhe_api.cu", "fedhe_noalloc.cu"]
+                "fedhe_mask.cu", "fedhe_api.cu", "fedhe_noalloc.cu", "fedhe_tokens.cu", "fedhe_norm.cu", "fedhe_linear.cu", "fedhe_map_api.cu"]
 HOST_SOURCES = ["fedhe_host.cpp"]
 HEADERS = ["fedhe_device.cuh", "fedhe_ntt.cuh", "fedhe_fft.cuh", "fedhe_internal.cuh", "fedhe_launch.h", "fedhe_host.h",
-           "fedhe_kernels.cuh", "fedhe_gauss.cuh", "fedhe_slots.cuh",
+           "fedhe_kernels.cuh", "fedhe_gauss.cuh", "fedhe_slots.cuh", "fedhe_map.cuh", "fedhe_map.h",
            os.path.join("..", "..", "include", "fedhe.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

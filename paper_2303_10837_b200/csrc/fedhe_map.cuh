@@ -1,0 +1,99 @@
+// What the kernels of the sensitivity map share (fedhe_tokens.cu, fedhe_norm.cu, fedhe_linear.cu): element types, loads of
+// rows at any alignment, sums over a warp.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "fedhe_kernels.cuh"
+#include "fedhe_map.h"
+
+namespace fedhe {
+
+template <class T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <>
+__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <class T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// V elements that one access moves: 16 bytes, or a single element where rows are not aligned to that.
+template <class T, int V>
+struct alignas(V * sizeof(T)) Pack {
+    T v[V];
+};
+template <class T>
+constexpr int WIDE = 16 / sizeof(T);
+
+template <class T, int V>
+__device__ __forceinline__ Pack<T, V> load_pack(const T *p) {
+    return *reinterpret_cast<const Pack<T, V> *>(p);
+}
+template <class T, int V>
+__device__ __forceinline__ void store_pack(T *p, const Pack<T, V> &a) {
+    *reinterpret_cast<Pack<T, V> *>(p) = a;
+}
+
+// a weight of a type that is known at run time (they are read once per thread block)
+__device__ __forceinline__ float load_weight(const void *p, int dtype, size_t i) {
+    return dtype == HE_F32    ? static_cast<const float *>(p)[i]
+           : dtype == HE_BF16 ? to_f32(static_cast<const __nv_bfloat16 *>(p)[i])
+                              : to_f32(static_cast<const __half *>(p)[i]);
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// The larger one; NaN where one of them is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// Where sample k ends that a row belongs to.  Offsets come from the caller's device memory: whatever they say, `k` stays below
+// `count`, and rows that no sample holds have k == count.
+struct SampleWalk {
+    const int32_t *offsets;
+    uint32_t count, k;
+    int64_t begin, end;      // of sample k
+    // the first sample that ends behind `row`
+    __device__ __forceinline__ void seek(const int32_t *off, uint32_t n, int64_t row) {
+        offsets = off;
+        count = n;
+        uint32_t lo = 0, hi = n;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if ((int64_t)__ldg(off + mid + 1) > row) hi = mid;
+            else lo = mid + 1;
+        }
+        k = lo;
+        bounds();
+    }
+    __device__ __forceinline__ void bounds() {
+        begin = k < count ? (int64_t)__ldg(offsets + k) : INT64_MAX;
+        end = k < count ? (int64_t)__ldg(offsets + k + 1) : INT64_MAX;
+    }
+    __device__ __forceinline__ void next(int64_t row) {      // the next one that ends behind `row`
+        do {
+            k++;
+            bounds();
+        } while (k < count && end <= row);
+    }
+};
+
+}  // namespace fedhe

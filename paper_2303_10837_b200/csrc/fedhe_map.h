@@ -1,0 +1,102 @@
+// Launch wrappers of the sensitivity map's kernels, called by fedhe_map_api.cu after it has checked the arguments.  All of them
+// enqueue work on `s` and return the launch status; none synchronises or allocates.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/fedhe.h"
+
+namespace fedhe {
+
+// A row-major matrix; `stride` is the distance of its rows in elements.
+struct MatArg {
+    const void *p;
+    size_t stride;
+};
+struct MatOut {
+    void *p;
+    size_t stride;
+};
+
+struct LogProbsArgs {
+    MatArg logits;
+    size_t rows, vocab;
+    const int64_t *targets;
+    uint32_t top;
+    float *logp, *lse, *entropy, *top_logp;
+    int64_t *top_ids;
+};
+cudaError_t launch_log_probs(const LogProbsArgs &a, int dtype, int n_sm, cudaStream_t s);
+
+struct LogProbsGradArgs {
+    MatArg logits;
+    size_t rows, vocab;
+    const int64_t *targets;
+    const float *lse, *entropy, *dlogp, *dentropy;
+    uint32_t top;
+    const int64_t *top_ids;
+    const float *dtop;
+    MatOut dlogits;
+};
+cudaError_t launch_log_probs_grad(const LogProbsGradArgs &a, int dtype, int n_sm, cudaStream_t s);
+
+struct NormArgs {
+    MatArg x;
+    size_t rows, width;
+    const void *weight, *bias;
+    int weight_type;
+    float eps;
+    MatOut y;
+    float *mean, *rstd;
+};
+cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, cudaStream_t s);
+
+// How rows are summed: all of them, or within a sample with the magnitudes added over the samples, or every row a sample of its own.
+enum class SumOver { ALL, SAMPLES, ROWS };
+
+struct NormGradArgs {
+    MatArg dy, x;
+    size_t rows, width;
+    const float *mean, *rstd;
+    const void *weight;
+    int weight_type;
+    SumOver over;
+    const int32_t *offsets;
+    uint32_t samples;
+    MatOut dx;
+    float *dweight, *dbias;
+    void *work;
+};
+size_t norm_grad_work_bytes(size_t rows, size_t width, int n_sm);
+cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, cudaStream_t s);
+
+// Sums of the columns of a matrix, dst (+)= the sums; work of column_sums_work_bytes()
+struct ColumnSumArgs {
+    MatArg m;
+    size_t rows, width;
+    SumOver over;
+    const int32_t *offsets;
+    uint32_t samples;
+    bool accumulate;
+    float *dst;
+    void *work;
+};
+size_t column_sums_work_bytes(size_t rows, size_t width, int n_sm);
+cudaError_t launch_column_sums(const ColumnSumArgs &a, int dtype, int n_sm, cudaStream_t s);
+
+struct LinearMapArgs {
+    MatArg x, dy;
+    size_t rows, inputs, outputs;
+    SumOver over;                  // SAMPLES or ROWS
+    const int32_t *offsets;
+    uint32_t samples;
+    bool accumulate;
+    float *weight, *bias;          // bias may be null
+    void *work;
+};
+size_t linear_map_work_bytes(const LinearMapArgs &a, int dtype, int n_sm);
+cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, cudaStream_t s);
+
+}  // namespace fedhe
