@@ -430,8 +430,14 @@ int he_layer_norm_backward(he_ctx *ctx, const void *dy_dev, size_t dy_stride, co
  *   bias[o]      = sum_k |sum_{t in k} dy[t][o]|.
  * samples_dev == NULL: every row is a sample of its own.  weight: dev float
  * [outputs][inputs], bias: dev float [outputs] or NULL; overwritten, or added
- * to if accumulate is not 0. */
-size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs);
+ * to if accumulate is not 0.
+ * Scratch: `samples`: whether the call has samples; `aligned`: whether every
+ * row of x and of dy begins on a 16-byte boundary (their strides are then at
+ * least their widths).  HE_F32 operands, magnitudes of rows and rows at other
+ * addresses are laid out there first.  fp32 products are taken from all 24 bits
+ * of either factor. */
+size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs,
+                                        int samples, int aligned);
 int he_linear_sensitivity(he_ctx *ctx, const void *x_dev, size_t x_stride, const void *dy_dev, size_t dy_stride, int dtype,
                           size_t rows, size_t inputs, size_t outputs, const int32_t *samples_dev, size_t num_samples,
                           int accumulate, float *weight_dev, float *bias_dev, void *work_dev, size_t work_bytes,

@@ -93,7 +93,7 @@ _SIGS = {
     "he_layer_norm_backward_work_bytes": (_sz, [_vp, _sz, _sz]),
     "he_layer_norm_backward": (C.c_int, [_vp, _vp, _sz, _vp, _sz, C.c_int, _sz, _sz, _vp, _vp, _vp, C.c_int, _vp, _sz, _vp, _sz, _vp, _vp,
                                          _vp, _sz, _vp]),
-    "he_linear_sensitivity_work_bytes": (_sz, [_vp, C.c_int, _sz, _sz, _sz]),
+    "he_linear_sensitivity_work_bytes": (_sz, [_vp, C.c_int, _sz, _sz, _sz, C.c_int, C.c_int]),
     "he_linear_sensitivity": (C.c_int, [_vp, _vp, _sz, _vp, _sz, C.c_int, _sz, _sz, _sz, _vp, _sz, C.c_int, _vp, _vp, _vp, _sz, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
@@ -731,6 +731,10 @@ def he_layer_norm_backward(ctx: Ctx, dy: torch.Tensor, x: torch.Tensor, mean: to
     return dx, dweight, dbias
 
 
+def _rows_aligned(t: torch.Tensor, stride: int, width: int) -> bool:
+    return stride >= width and t.data_ptr() % 16 == 0 and stride * t.element_size() % 16 == 0
+
+
 def he_linear_sensitivity(ctx: Ctx, x: torch.Tensor, dy: torch.Tensor, samples: Optional[torch.Tensor] = None,
                           out: Optional[torch.Tensor] = None, out_bias: Optional[torch.Tensor] = None, accumulate: bool = False,
                           bias: bool = True):
@@ -758,7 +762,8 @@ def he_linear_sensitivity(ctx: Ctx, x: torch.Tensor, dy: torch.Tensor, samples: 
         out = torch.empty((outputs, inputs), dtype=torch.float32, device=x.device)
     if bias and out_bias is None:
         out_bias = torch.empty(outputs, dtype=torch.float32, device=x.device)
-    room = _lib.he_linear_sensitivity_work_bytes(ctx.handle, code, rows, inputs, outputs)
+    aligned = _rows_aligned(x, stride, inputs) and _rows_aligned(dy, dy_stride, outputs)
+    room = _lib.he_linear_sensitivity_work_bytes(ctx.handle, code, rows, inputs, outputs, samples is not None, aligned)
     work = torch.empty(max(room, 16), dtype=torch.uint8, device=x.device)
     _check(_lib.he_linear_sensitivity(ctx.handle, _ptr(x), stride, _ptr(dy), dy_stride, code, rows, inputs, outputs, _ptr(samples), count,
                                       1 if accumulate else 0, _ptr(out), _ptr(out_bias) if bias else None, _ptr(work), work.numel(), _stream()),

@@ -1,82 +1,604 @@
 // A linear layer's entries of the sensitivity map:  S[o][i] = sum_k |sum_{t in k} dy[t][o] x[t][i]|  over the samples k, without the
 // samples' gradients ever being in memory; every row a sample of its own:  S = |dy|^T |x|.
+//
+// A product of tiles on the tensor cores whose contracted index is the row.  Both operands lie in memory as the tensor cores want
+// them with the contracted index second ("MN-major"), so tiles come by TMA and nothing is transposed.  A sample's product is summed in tensor
+// memory; the epilogue's warps add its magnitudes to sums that they hold in registers, while the next sample goes to the other half of
+// tensor memory.  Only the finished sums leave the chip.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
 #include "fedhe_map.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace fedhe {
 
 namespace {
 
-constexpr int TILE = 64, DEPTH = 16;
+constexpr uint32_t DEPTH = 64;                          // rows of a stage
+constexpr uint32_t GROUP = 64, GROUP_BYTES = DEPTH * 128;  // columns of a swizzled group, 128 bytes of each row
+constexpr uint32_t MOST_N = 256;                        // inputs of a tile; its outputs are the 128 lanes of tensor memory of each block
+// Tensor memory adds without rounding to nearest, so that a long sum loses 2^-24 of itself for each step of 16 rows: pieces of
+// so many rows are summed there, and their sums added in fp32.
+constexpr uint32_t PIECE = 512;
+constexpr uint32_t THREADS = 384;                       // warps: loads, products, two between them, eight of the epilogue
+constexpr uint32_t STAGING = 128 * (MOST_N + 1) * 4;
+constexpr uint32_t TRIES = 256;                         // of 10 ms at most
 
-template <class T>
-__global__ void __launch_bounds__(256) linear_map_kernel(const LinearMapArgs a) {
-    __shared__ float g[DEPTH][TILE + 4], x[DEPTH][TILE + 4];
-    const uint32_t tid = threadIdx.x, ty = tid / 16, tx = tid % 16;
-    const size_t o0 = (size_t)blockIdx.y * TILE, i0 = (size_t)blockIdx.x * TILE;
-    const bool rows_alone = a.over == SumOver::ROWS;
-    float total[4][4] = {};
-    const uint32_t samples = rows_alone ? 1 : a.samples;
-    int64_t lo = 0, hi = 0;
-    for (uint32_t k = 0; k < samples; k++) {
-        if (rows_alone) {
-            hi = (int64_t)a.rows;
-        } else {                                         // whatever the offsets say, rows lie within the matrices
-            lo = max((int64_t)a.offsets[k], hi);
-            hi = min(max((int64_t)a.offsets[k + 1], lo), (int64_t)a.rows);
-        }
-        float acc[4][4] = {};
-        for (int64_t r0 = lo; r0 < hi; r0 += DEPTH) {
-            for (uint32_t i = tid; i < DEPTH * TILE; i += 256) {
-                const int64_t r = r0 + i / TILE;
-                const size_t c = i % TILE;
-                float gv = 0.0f, xv = 0.0f;
-                if (r < hi && o0 + c < a.outputs) gv = to_f32(static_cast<const T *>(a.dy.p)[(size_t)r * a.dy.stride + o0 + c]);
-                if (r < hi && i0 + c < a.inputs) xv = to_f32(static_cast<const T *>(a.x.p)[(size_t)r * a.x.stride + i0 + c]);
-                g[i / TILE][c] = rows_alone ? fabsf(gv) : gv;
-                x[i / TILE][c] = rows_alone ? fabsf(xv) : xv;
-            }
-            __syncthreads();
-#pragma unroll
-            for (int d = 0; d < DEPTH; d++)
-#pragma unroll
-                for (int p = 0; p < 4; p++)
-#pragma unroll
-                    for (int q = 0; q < 4; q++) acc[p][q] = fmaf(g[d][ty * 4 + p], x[d][tx * 4 + q], acc[p][q]);
-            __syncthreads();
-        }
-#pragma unroll
-        for (int p = 0; p < 4; p++)
-#pragma unroll
-            for (int q = 0; q < 4; q++) total[p][q] += fabsf(acc[p][q]);
+// ---- the hardware's instructions ----
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
+}
+// arrives at a barrier of the block `rank` of the cluster
+__device__ __forceinline__ void bar_arrive(uint64_t *b, uint32_t rank) {
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_at(b)),
+                 "r"(rank)
+                 : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_at(b)), "r"(bytes) : "memory");
+}
+// By a whole warp; false after TRIES: something that should have come did not.
+__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity) {
+    for (uint32_t i = 0; i < TRIES; i++) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(smem_at(b)), "r"(parity)
+                     : "memory");
+        if (__all_sync(0xffffffffu, done)) return true;
     }
+    return false;
+}
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, int32_t col, int32_t row, int32_t part, uint64_t *bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to), "l"(map),
+                 "r"(col), "r"(row), "r"(part), "r"(smem_at(bar))
+                 : "memory");
+}
+// An operand in shared memory whose rows (the contracted index) are 128 bytes of a group of 64 columns, swizzled in atoms of eight rows: groups
+// are GROUP_BYTES apart, atoms 1024.
+__device__ __forceinline__ uint64_t operand(uint32_t at) {
+    return (uint64_t)((at >> 4) & 0x3fff) | (uint64_t)(GROUP_BYTES >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+template <int CG>
+__device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(what), "r"((uint32_t)add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(what), "r"((uint32_t)add)
+                     : "memory");
+}
+// the products issued so far arrive at a barrier when they are done, in both blocks of a pair
+template <int CG>
+__device__ __forceinline__ void commit(uint64_t *bar, uint16_t blocks) {
+    if (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_at(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_at(bar)), "h"(blocks)
+                     : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void tmem_take(uint32_t *where) {
+    if (CG == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(where)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(where)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void tmem_give(uint32_t at) {
+    if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(at));
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(at));
+}
+__device__ __forceinline__ void tmem_order_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_order_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+#define REGS16(v, o)                                                                                                                          \
+    "=f"(v[o + 0]), "=f"(v[o + 1]), "=f"(v[o + 2]), "=f"(v[o + 3]), "=f"(v[o + 4]), "=f"(v[o + 5]), "=f"(v[o + 6]), "=f"(v[o + 7]), "=f"(v[o + 8]), \
+        "=f"(v[o + 9]), "=f"(v[o + 10]), "=f"(v[o + 11]), "=f"(v[o + 12]), "=f"(v[o + 13]), "=f"(v[o + 14]), "=f"(v[o + 15])
+__device__ __forceinline__ void tmem_get32(uint32_t at, float (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : REGS16(v, 0), REGS16(v, 16)
+                 : "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_get16(uint32_t at, float (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : REGS16(v, 0)
+                 : "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_put16(uint32_t at, const float (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(at),
+                 "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]), "f"(v[11]),
+                 "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15])
+                 : "memory");
+}
+#undef REGS16
+
+// ---- what every role of a block goes through: the pieces of its samples ----
+
+struct Piece {
+    int32_t row, count;      // count > 0
+    bool first, last;        // of a sample
+};
+
+// By a whole warp; `offsets` null: the rows [lo, hi) by themselves, where any cut will do.
+struct Pieces {
+    const int32_t *offsets;
+    uint32_t k, end, base;
+    int32_t rows, held, lo, hi, at;
+    __device__ __forceinline__ int32_t offset(uint32_t i) {
+        if (i - base >= 32u) {
+            base = i;
+            const uint32_t j = min(i + (threadIdx.x & 31u), end);
+            held = __ldg(offsets + j);
+        }
+        const int32_t v = __shfl_sync(0xffffffffu, held, i - base);
+        return min(max(v, 0), rows);
+    }
+    __device__ __forceinline__ bool next(Piece &p) {
+        while (at >= hi) {
+            if (!offsets || k >= end) return false;
+            lo = offset(k);
+            hi = offset(k + 1);
+            at = lo;
+            k++;
+        }
+        p.row = at;
+        p.count = min((int32_t)PIECE, hi - at);
+        p.first = !offsets || at == lo;
+        at += p.count;
+        p.last = !offsets || at == hi;
+        return true;
+    }
+};
+// the first offset that is not below a row
+__device__ __forceinline__ uint32_t first_at(const int32_t *offsets, uint32_t count, int64_t row) {
+    uint32_t lo = 0, hi = count;
+    while (lo < hi) {
+        const uint32_t mid = (lo + hi) / 2;
+        if ((int64_t)__ldg(offsets + mid) >= row) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+struct LinearJob {
+    const int32_t *offsets;
+    uint32_t samples, rows, inputs, outputs;
+    uint32_t n, splits, tiles_i;      // inputs of a tile; blocks (or pairs) that share a tile's samples
+    uint32_t stages, pairs, what;     // products of pieces of fp32 operands: 6, or 1; the instruction's descriptor
+    bool accumulate;
+    float *weight;
+    int *status;
+};
+
+// Which pieces of fp32 values are multiplied, the smallest products first: all of them down to 2^-16 of the whole.
+__device__ __forceinline__ uint32_t piece_of_dy(uint32_t pair) { return (0x001120u >> (pair * 4)) & 3u; }   // 0 2 1 1 0 0 from pair 0 on
+__device__ __forceinline__ uint32_t piece_of_x(uint32_t pair) { return (0x010102u >> (pair * 4)) & 3u; }    // 2 0 1 0 1 0
+
+// Of a cluster of splits * CG blocks, CG blocks work on a tile of CG * 128 outputs and n inputs: each holds 128 outputs' columns of dy
+// and n / CG inputs' columns of x, and the sums of its outputs.
+template <int CG>
+__global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_constant__ CUtensorMap dy64, const __grid_constant__ CUtensorMap dy16,
+                                                                const __grid_constant__ CUtensorMap x64, const __grid_constant__ CUtensorMap x16,
+                                                                const LinearJob job) {
+    extern __shared__ uint8_t raw[];
+    constexpr uint32_t MOST_STAGES = 12;
+    __shared__ uint64_t full[MOST_STAGES], ready[MOST_STAGES], empty[MOST_STAGES], sum_full[2], sum_empty[2], drained;
+    __shared__ uint32_t tmem_base;
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid & 31u;
+    const uint32_t rank = cluster.block_rank(), half = rank % CG, leader = rank - half, split = rank / CG;
+    const uint32_t tile = blockIdx.x / (job.splits * CG);
+    const uint32_t o0 = (tile / job.tiles_i) * 128 * CG + half * 128, i0 = (tile % job.tiles_i) * job.n;
+    const uint32_t nb = job.n / CG, ib = i0 + half * nb;                       // x's columns in this block
+    // groups of 64 columns that hold anything; what multiplies the others lies outside the result
+    const uint32_t ga = o0 >= job.outputs ? 0 : min(2u, (job.outputs - o0 + GROUP - 1) / GROUP);
+    const uint32_t gb = ib >= job.inputs ? 0 : min((nb + GROUP - 1) / GROUP, (job.inputs - ib + GROUP - 1) / GROUP);
+    const uint32_t smem = (smem_at(raw) + 1023u) & ~1023u;
+    const uint32_t a_bytes = 2 * GROUP_BYTES, stage_bytes = a_bytes + (nb + GROUP - 1) / GROUP * GROUP_BYTES;
+    if (tid == 0) {
+        for (uint32_t s = 0; s < job.stages; s++) {
+            bar_init(&full[s], 1);
+            bar_init(&ready[s], CG);
+            bar_init(&empty[s], 1);
+        }
+        for (int b = 0; b < 2; b++) {
+            bar_init(&sum_full[b], 1);
+            bar_init(&sum_empty[b], 8 * CG);
+        }
+        bar_init(&drained, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_take<CG>(&tmem_base);
+    tmem_order_before();
+    cluster.sync();
+    tmem_order_after();
+    const uint32_t tmem = tmem_base;
+
+    Pieces pieces{job.offsets, 0, 0, 0x80000000u, (int32_t)job.rows, 0, 0, 0, 0};
+    const int64_t r0 = (int64_t)job.rows * split / job.splits, r1 = (int64_t)job.rows * (split + 1) / job.splits;
+    if (job.offsets) {
+        // a sample goes to the split in whose share of the rows it begins
+        pieces.k = split == 0 ? 0 : first_at(job.offsets, job.samples, r0);
+        pieces.end = split + 1 == job.splits ? job.samples : first_at(job.offsets, job.samples, r1);
+    } else {
+        pieces.lo = pieces.at = (int32_t)r0;
+        pieces.hi = (int32_t)r1;
+    }
+    Piece p;
+    bool well = true;
+    float total[4][32];                                                        // of the epilogue's warps
+    if (warp == 0) {
+        uint32_t s = 0, turn = 0;
+        while (well && pieces.next(p))
+            for (uint32_t q = 0; well && q < job.pairs; q++) {
+                const int32_t pa = job.pairs == 1 ? 0 : (int32_t)piece_of_dy(q), pb = job.pairs == 1 ? 0 : (int32_t)piece_of_x(q);
+                for (int32_t r = 0; well && r < p.count; r += DEPTH) {
+                    well = bar_wait(&empty[s], (turn & 1u) ^ 1u);
+                    if (!well) break;
+                    if (lane == 0) {
+                        const uint32_t at = smem + s * stage_bytes;
+                        const uint32_t sixteens = min(4u, (uint32_t)(p.count - r + 15) / 16);
+                        bar_expect(&full[s], (ga + gb) * sixteens * 16 * 128);
+                        const int32_t row = p.row + r;
+                        if (sixteens == 4) {
+                            for (uint32_t g = 0; g < ga; g++) tma_load(at + g * GROUP_BYTES, &dy64, (int32_t)(o0 + g * GROUP), row, pa, &full[s]);
+                            for (uint32_t g = 0; g < gb; g++) tma_load(at + a_bytes + g * GROUP_BYTES, &x64, (int32_t)(ib + g * GROUP), row, pb, &full[s]);
+                        } else {
+                            for (uint32_t h = 0; h < sixteens; h++) {
+                                for (uint32_t g = 0; g < ga; g++)
+                                    tma_load(at + g * GROUP_BYTES + h * 2048, &dy16, (int32_t)(o0 + g * GROUP), row + (int32_t)h * 16, pa, &full[s]);
+                                for (uint32_t g = 0; g < gb; g++)
+                                    tma_load(at + a_bytes + g * GROUP_BYTES + h * 2048, &x16, (int32_t)(ib + g * GROUP), row + (int32_t)h * 16, pb, &full[s]);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    if (++s == job.stages) s = 0, turn++;
+                }
+            }
+        // no copy is under way when the block ends: the last of each stage is waited for, whatever happened
+        for (uint32_t i = 0; i < job.stages; i++)
+            if (turn || i < s) {
+                const uint32_t last = i < s ? turn : turn - 1;
+                if (!bar_wait(&full[i], last & 1u)) well = false;
+            }
+    } else if (warp == 1) {
+        if (half == 0) {
+            uint32_t s = 0, turn = 0, uses[2] = {0, 0}, held = 1;
+            while (well && pieces.next(p)) {
+                if (p.first) held ^= 1;
+                const uint32_t b = p.first ? held : held ^ 1;
+                const uint32_t use = b ? uses[1]++ : uses[0]++;
+                well = bar_wait(&sum_empty[b], (use & 1u) ^ 1u);
+                tmem_order_after();
+                const uint32_t d = tmem + b * MOST_N;
+                bool add = false;
+                for (uint32_t q = 0; well && q < job.pairs; q++)
+                    for (int32_t r = 0; well && r < p.count; r += DEPTH) {
+                        well = bar_wait(&ready[s], turn & 1u);
+                        if (!well) break;
+                        tmem_order_after();
+                        if (lane == 0) {
+                            const uint32_t at = smem + s * stage_bytes;
+                            const uint32_t sixteens = min(4u, (uint32_t)(p.count - r + 15) / 16);
+                            for (uint32_t h = 0; h < sixteens; h++) {
+                                multiply<CG>(d, operand(at + h * 2048), operand(at + a_bytes + h * 2048), job.what, add);
+                                add = true;
+                            }
+                            commit<CG>(&empty[s], (uint16_t)(3u << leader));
+                        }
+                        add = true;
+                        __syncwarp();
+                        if (++s == job.stages) s = 0, turn++;
+                    }
+                if (lane == 0 && well) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
+                __syncwarp();
+            }
+            // products under way use both blocks' memory
+            if (lane == 0) commit<CG>(&drained, (uint16_t)(3u << leader));
+            __syncwarp();
+        }
+        if (!bar_wait(&drained, 0)) well = false;
+    } else if (warp < 4) {
+        // Rows of the next sample, or none of any, that came with a sample's last ones count as zeros.  The two warps take stages in turn.
+        uint32_t s = 0, turn = 0, i = 0;
+        while (well && pieces.next(p))
+            for (uint32_t q = 0; well && q < job.pairs; q++)
+                for (int32_t r = 0; well && r < p.count; r += DEPTH, i++) {
+                    if ((i & 1u) == warp - 2) {
+                        well = bar_wait(&full[s], turn & 1u);
+                        if (!well) break;
+                        const uint32_t left = (uint32_t)min((int32_t)DEPTH, p.count - r);
+                        if (left & 15u) {
+                            const uint32_t at = smem + s * stage_bytes + left * 128, words = (16 - (left & 15u)) * 8;
+                            for (uint32_t w = lane; w < words; w += 32) {
+                                for (uint32_t g = 0; g < ga; g++)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
+                                for (uint32_t g = 0; g < gb; g++)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + a_bytes + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
+                            }
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        }
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(&ready[s], leader);
+                    }
+                    if (++s == job.stages) s = 0, turn++;
+                }
+    } else {
 #pragma unroll
-    for (int p = 0; p < 4; p++)
+        for (int j = 0; j < 4; j++)
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-            const size_t o = o0 + ty * 4 + p, i = i0 + tx * 4 + q;
-            if (o < a.outputs && i < a.inputs) {
-                float *d = a.weight + o * a.inputs + i;
-                *d = a.accumulate ? *d + total[p][q] : total[p][q];
+            for (int e = 0; e < 32; e++) total[j][e] = 0.0f;
+        const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - 4) / 4 * cols;
+        uint32_t uses[2] = {0, 0}, held = 1;
+        while (well && pieces.next(p)) {
+            if (p.first) held ^= 1;
+            const uint32_t b = p.first ? held : held ^ 1;
+            const uint32_t use = b ? uses[1]++ : uses[0]++;
+            well = bar_wait(&sum_full[b], use & 1u);
+            if (!well) break;
+            tmem_order_after();
+            if (p.first && p.last) {
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (j * 32 < cols) {
+                        float v[32];
+                        tmem_get32(mine + b * MOST_N + j * 32, v);
+#pragma unroll
+                        for (int e = 0; e < 32; e++) total[j][e] += fabsf(v[e]);
+                    }
+            } else if (!p.first) {
+                // a long sample: its first piece's place holds the sum of its pieces
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    if (j * 16 < cols) {
+                        float v[16], u[16];
+                        tmem_get16(mine + b * MOST_N + j * 16, v);
+                        tmem_get16(mine + held * MOST_N + j * 16, u);
+#pragma unroll
+                        for (int e = 0; e < 16; e++) u[e] += v[e];
+                        if (p.last) {
+#pragma unroll
+                            for (int e = 0; e < 16; e++) total[j / 2][j % 2 * 16 + e] += fabsf(u[e]);
+                        } else {
+                            tmem_put16(mine + held * MOST_N + j * 16, u);
+                        }
+                    }
+            }
+            tmem_order_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (!p.first || p.last) bar_arrive(&sum_empty[b], leader);
+                if (!p.first && p.last) bar_arrive(&sum_empty[held], leader);
             }
         }
+    }
+    if (!well && lane == 0) atomicOr(job.status, STATUS_COPY);
+    // every product of the pair is done: the stages' memory takes the sums
+    __syncthreads();
+    cluster.sync();
+    if (warp == 1) {
+        tmem_order_after();
+        tmem_give<CG>(tmem);
+    }
+    float *sums = reinterpret_cast<float *>(raw + (smem - smem_at(raw)));
+    const uint32_t pitch = job.n + 1;
+    if (warp >= 4) {
+        float *to = sums + ((warp & 3u) * 32 + lane) * pitch + (warp - 4) / 4 * (job.n / 2);
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            if (j * 32 < job.n / 2)
+#pragma unroll
+                for (int e = 0; e < 32; e++) to[j * 32 + e] = total[j][e];
+    }
+    cluster.sync();
+    // the splits' sums, each block some outputs of its 128
+    const uint32_t first = 128 * split / job.splits, behind = 128 * (split + 1) / job.splits;
+    const uint32_t width = min(job.n, job.inputs - i0);
+    for (uint32_t o = first + warp; o < behind; o += THREADS / 32) {
+        if (o0 + o >= job.outputs) break;
+        float *out = job.weight + (size_t)(o0 + o) * job.inputs + i0;
+        for (uint32_t c = lane; c < width; c += 32) {
+            float v = 0.0f;
+            for (uint32_t f = 0; f < job.splits; f++) v += *cluster.map_shared_rank(sums + o * pitch + c, f * CG + half);
+            out[c] = job.accumulate ? out[c] + v : v;
+        }
+    }
+    cluster.sync();                          // nobody leaves while its memory is read
+}
+
+// ---- operands that TMA cannot take as they are ----
+
+// The values v as the tensor cores take them: bf16 or fp16 as they are, fp32 as three bf16 pieces whose sum is v (each the rounding
+// of what the pieces before it leave; an infinity or a NaN is its own first piece).  Magnitudes where rows are samples of their own.
+struct StageArgs {
+    MatArg in[2];
+    uint32_t width[2], pitch[2];
+    uint16_t *out[2];
+    uint32_t rows;
+    bool magnitudes;
+};
+template <class T>
+__global__ void __launch_bounds__(256) stage_kernel(const StageArgs a) {
+    constexpr int PIECES = sizeof(T) == 4 ? 3 : 1;
+    const int m = blockIdx.y;
+    const uint32_t width = a.width[m], pitch = a.pitch[m], packs = pitch / 8;
+    const size_t plane = (size_t)a.rows * pitch, all = (size_t)a.rows * packs;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
+        const size_t r = i / packs;
+        const uint32_t c = (uint32_t)(i % packs) * 8;
+        const T *in = static_cast<const T *>(a.in[m].p) + r * a.in[m].stride + c;
+        Pack<uint16_t, 8> o[PIECES];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            T v = c + e < width ? in[e] : T(0);
+            if constexpr (PIECES == 1) {
+                uint16_t b;
+                memcpy(&b, &v, 2);
+                o[0].v[e] = a.magnitudes ? b & 0x7fffu : b;
+            } else {
+                float left = a.magnitudes ? fabsf(v) : v;
+#pragma unroll
+                for (int q = 0; q < 3; q++) {
+                    __nv_bfloat16 b = __float2bfloat16_rn(left);
+                    // what rounds up to infinity is cut instead
+                    if (__hisinf(b) && !isinf(left)) b = __float2bfloat16_rz(left);
+                    o[q].v[e] = __bfloat16_as_ushort(b);
+                    left = isfinite(left) ? left - __bfloat162float(b) : 0.0f;
+                }
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < PIECES; q++) store_pack<uint16_t, 8>(a.out[m] + q * plane + r * pitch + c, o[q]);
+    }
+}
+
+inline uint32_t pitch_of(size_t width) { return (uint32_t)((width + 7) / 8 * 8); }
+inline size_t staged_words(size_t rows, size_t width, int dtype) { return (rows * pitch_of(width) * (dtype == HE_F32 ? 3 : 1) + 127) / 128 * 128; }
+
+// ---- launch ----
+
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+Encode tensor_map_encoder() {
+    static const Encode got = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) f = nullptr;
+        return reinterpret_cast<Encode>(f);
+    }();
+    return got;
+}
+
+// boxes of 64 columns and `box` rows of a matrix of 16-bit elements in `parts` planes
+bool tensor_map(CUtensorMap &m, const void *p, size_t width, size_t rows, size_t stride, uint32_t parts, bool half, uint32_t box) {
+    const Encode encode = tensor_map_encoder();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {width, rows, parts}, strides[2] = {stride * 2, parts == 1 ? stride * 2 : rows * stride * 2};
+    const cuuint32_t boxes[3] = {GROUP, box, 1}, steps[3] = {1, 1, 1};
+    return encode(&m, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(p), dims, strides, boxes, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How a product is shared out.
+struct Plan {
+    uint32_t cg, n, splits;
+};
+Plan plan_of(const LinearMapArgs &a, uint32_t pairs, int n_sm) {
+    Plan best{1, 64, 1};
+    double least = 1e300;
+    for (uint32_t cg = 1; cg <= 2; cg++)
+        for (uint32_t n = 64 * cg; n <= MOST_N; n += 64 * cg)
+            for (uint32_t c = 1; c * cg <= 8; c++) {
+                if (c > 1 && c > (a.over == SumOver::SAMPLES ? (size_t)a.samples : (a.rows + DEPTH - 1) / DEPTH)) break;
+                const double tiles = (double)((a.outputs + 128 * cg - 1) / (128 * cg)) * (double)((a.inputs + n - 1) / n);
+                const double waves = ceil(tiles * cg * c / n_sm);
+                // clocks of a row: its products, or its bytes at what L2 gives an SM
+                const double row = fmax(n / 32.0, (128.0 + n / cg) * 2 / 48);
+                const double t = waves * ((double)a.rows / c * pairs * row + 4000 + 8.0 * n + (c > 1 ? 1500 : 0));
+                if (t < least) least = t, best = Plan{cg, n, c};
+            }
+    return best;
+}
+
+template <int CG>
+cudaError_t launch(const CUtensorMap (&m)[4], const LinearJob &job, uint32_t tiles, cudaStream_t s) {
+    const uint32_t stage = 2 * GROUP_BYTES + (job.n / CG + GROUP - 1) / GROUP * GROUP_BYTES;
+    const uint32_t bytes = (job.stages * stage > STAGING ? job.stages * stage : STAGING) + 1024;
+    cudaError_t rc = cudaFuncSetAttribute(linear_map_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (rc != cudaSuccess) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(tiles * job.splits * CG);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim = {job.splits * CG, 1, 1};
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    rc = cudaLaunchKernelEx(&cfg, linear_map_kernel<CG>, m[0], m[1], m[2], m[3], job);
+    return rc != cudaSuccess ? rc : FEDHE_LAUNCHED();
 }
 
 }  // namespace
 
-size_t linear_map_work_bytes(const LinearMapArgs &a, int dtype, int n_sm) {
-    (void)dtype;
-    return a.bias ? column_sums_work_bytes(a.rows, a.outputs, n_sm) : 0;
+bool linear_map_aligned(const MatArg &m, size_t width, int dtype) {
+    return dtype != HE_F32 && reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.stride % 8 == 0 && m.stride >= width;
 }
 
-cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, cudaStream_t s) {
-    const dim3 grid(blocks_for(a.inputs, TILE), blocks_for(a.outputs, TILE));
-    if (dtype == HE_F32) linear_map_kernel<float><<<grid, 256, 0, s>>>(a);
-    else if (dtype == HE_BF16) linear_map_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(a);
-    else linear_map_kernel<__half><<<grid, 256, 0, s>>>(a);
-    const cudaError_t rc = FEDHE_LAUNCHED();
-    if (rc != cudaSuccess || !a.bias) return rc;
-    const ColumnSumArgs b{a.dy, a.rows, a.outputs, a.over, a.offsets, a.samples, a.accumulate, a.bias, a.work};
-    return launch_column_sums(b, dtype, n_sm, s);
+size_t linear_map_work_bytes(size_t rows, size_t inputs, size_t outputs, int dtype, bool samples, bool aligned, bool bias, int n_sm) {
+    size_t bytes = bias ? (column_sums_work_bytes(rows, outputs, n_sm) + 255) / 256 * 256 : 0;
+    if (!samples || !aligned) bytes += (staged_words(rows, inputs, dtype) + staged_words(rows, outputs, dtype)) * 2;
+    return bytes;
+}
+
+cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *status, cudaStream_t s) {
+    uint8_t *work = static_cast<uint8_t *>(a.work);
+    if (a.bias) {
+        const ColumnSumArgs b{a.dy, a.rows, a.outputs, a.over, a.offsets, a.samples, a.accumulate, a.bias, work};
+        const cudaError_t rc = launch_column_sums(b, dtype, n_sm, s);
+        if (rc != cudaSuccess) return rc;
+        work += (column_sums_work_bytes(a.rows, a.outputs, n_sm) + 255) / 256 * 256;
+    }
+    if (!a.rows) return a.accumulate ? cudaSuccess : cudaMemsetAsync(a.weight, 0, a.inputs * a.outputs * sizeof(float), s);
+    const bool alone = a.over == SumOver::ROWS;
+    MatArg x = a.x, dy = a.dy;
+    uint32_t parts = 1;
+    if (alone || !linear_map_aligned(a.x, a.inputs, dtype) || !linear_map_aligned(a.dy, a.outputs, dtype)) {
+        uint16_t *to = reinterpret_cast<uint16_t *>(work);
+        const StageArgs g{{a.x, a.dy}, {(uint32_t)a.inputs, (uint32_t)a.outputs}, {pitch_of(a.inputs), pitch_of(a.outputs)}, {to, to + staged_words(a.rows, a.inputs, dtype)},
+                          (uint32_t)a.rows, alone};
+        const size_t packs = a.rows * (size_t)(g.pitch[0] > g.pitch[1] ? g.pitch[0] : g.pitch[1]) / 8, most = (size_t)16 * n_sm;
+        const dim3 grid((unsigned)((packs + 255) / 256 < most ? (packs + 255) / 256 : most), 2);
+        if (dtype == HE_F32) stage_kernel<float><<<grid, 256, 0, s>>>(g);
+        else stage_kernel<uint16_t><<<grid, 256, 0, s>>>(g);
+        const cudaError_t rc = FEDHE_LAUNCHED();
+        if (rc != cudaSuccess) return rc;
+        x = MatArg{g.out[0], g.pitch[0]};
+        dy = MatArg{g.out[1], g.pitch[1]};
+        parts = dtype == HE_F32 ? 3 : 1;
+    }
+    const uint32_t pairs = parts == 3 ? 6 : 1;
+    const Plan plan = plan_of(a, pairs, n_sm);
+    CUtensorMap m[4];
+    const bool half = dtype == HE_F16;
+    if (!tensor_map(m[0], dy.p, a.outputs, a.rows, dy.stride, parts, half, 64) || !tensor_map(m[1], dy.p, a.outputs, a.rows, dy.stride, parts, half, 16) ||
+        !tensor_map(m[2], x.p, a.inputs, a.rows, x.stride, parts, half, 64) || !tensor_map(m[3], x.p, a.inputs, a.rows, x.stride, parts, half, 16))
+        return cudaErrorInvalidValue;
+    const uint32_t stage = 2 * GROUP_BYTES + (plan.n / plan.cg + GROUP - 1) / GROUP * GROUP_BYTES;
+    LinearJob job{};
+    job.offsets = alone ? nullptr : a.offsets;
+    job.samples = a.samples;
+    job.rows = (uint32_t)a.rows;
+    job.inputs = (uint32_t)a.inputs;
+    job.outputs = (uint32_t)a.outputs;
+    job.n = plan.n;
+    job.splits = plan.splits;
+    job.tiles_i = (uint32_t)((a.inputs + plan.n - 1) / plan.n);
+    job.stages = 196608 / stage;
+    if (job.stages > 8) job.stages = 8;
+    job.pairs = pairs;
+    // fp32 sums; both operands fp16 or bf16, with the contracted index second; n columns, 128 rows for each block
+    const uint32_t type = half ? 0 : 1;
+    job.what = 1u << 4 | type << 7 | type << 10 | 1u << 15 | 1u << 16 | (plan.n >> 3) << 17 | (128 * plan.cg >> 4) << 24;
+    job.accumulate = a.accumulate;
+    job.weight = a.weight;
+    job.status = status;
+    const uint32_t tiles = (uint32_t)((a.outputs + 128 * plan.cg - 1) / (128 * plan.cg)) * job.tiles_i;
+    return plan.cg == 1 ? launch<1>(m, job, tiles, s) : launch<2>(m, job, tiles, s);
 }
 
 }  // namespace fedhe

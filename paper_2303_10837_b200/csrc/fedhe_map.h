@@ -96,7 +96,10 @@ struct LinearMapArgs {
     float *weight, *bias;          // bias may be null
     void *work;
 };
-size_t linear_map_work_bytes(const LinearMapArgs &a, int dtype, int n_sm);
-cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, cudaStream_t s);
+// whether the kernels can read a matrix where it lies
+bool linear_map_aligned(const MatArg &m, size_t width, int dtype);
+size_t linear_map_work_bytes(size_t rows, size_t inputs, size_t outputs, int dtype, bool samples, bool aligned, bool bias, int n_sm);
+// status: the context's, raised where something inside the kernel does not arrive
+cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 }  // namespace fedhe

@@ -101,16 +101,9 @@ int he_layer_norm_backward(he_ctx *ctx, const void *dy_dev, size_t dy_stride, co
     return done(launch_norm_grad(a, dtype, ctx->sm_count, as_stream(stream)));
 }
 
-static LinearMapArgs linear_args(const void *x, size_t x_stride, const void *dy, size_t dy_stride, size_t rows, size_t inputs, size_t outputs,
-                                 const int32_t *samples, size_t num_samples, int accumulate, float *weight, float *bias, void *work) {
-    return LinearMapArgs{{x, x_stride}, {dy, dy_stride}, rows, inputs, outputs, samples ? SumOver::SAMPLES : SumOver::ROWS, samples,
-                         (uint32_t)num_samples, accumulate != 0, weight, bias, work};
-}
-
-size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs) {
+size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs, int samples, int aligned) {
     if (!good(ctx) || !type_bytes(dtype) || !inputs || !outputs || !fits(rows, inputs) || !fits(rows, outputs)) return 0;
-    float some;                          // never touched: with a bias
-    return linear_map_work_bytes(linear_args(nullptr, inputs, nullptr, outputs, rows, inputs, outputs, nullptr, 0, 0, &some, &some, nullptr), dtype, ctx->sm_count);
+    return linear_map_work_bytes(rows, inputs, outputs, dtype, samples != 0, aligned != 0 && dtype != HE_F32, true, ctx->sm_count);
 }
 
 int he_linear_sensitivity(he_ctx *ctx, const void *x_dev, size_t x_stride, const void *dy_dev, size_t dy_stride, int dtype, size_t rows,
@@ -122,10 +115,12 @@ int he_linear_sensitivity(he_ctx *ctx, const void *x_dev, size_t x_stride, const
     if (rows && (!x_dev || !dy_dev)) return HE_ERR_INVALID_ARG;
     if (!natural(x_dev, w) || !natural(dy_dev, w) || !natural(samples_dev, 4) || !natural(weight_dev, 4) || !natural(bias_dev, 4) || !natural(work_dev, 16))
         return HE_ERR_INVALID_ARG;
-    const size_t need = he_linear_sensitivity_work_bytes(ctx, dtype, rows, inputs, outputs);
+    const bool aligned = linear_map_aligned({x_dev, x_stride}, inputs, dtype) && linear_map_aligned({dy_dev, dy_stride}, outputs, dtype);
+    const size_t need = linear_map_work_bytes(rows, inputs, outputs, dtype, samples_dev != nullptr, aligned, bias_dev != nullptr, ctx->sm_count);
     if (work_bytes < need || (need && !work_dev)) return HE_ERR_INVALID_ARG;
-    const LinearMapArgs a = linear_args(x_dev, x_stride, dy_dev, dy_stride, rows, inputs, outputs, samples_dev, num_samples, accumulate, weight_dev, bias_dev, work_dev);
-    return done(launch_linear_map(a, dtype, ctx->sm_count, as_stream(stream)));
+    const LinearMapArgs a{{x_dev, x_stride}, {dy_dev, dy_stride}, rows, inputs, outputs, samples_dev ? SumOver::SAMPLES : SumOver::ROWS, samples_dev,
+                          (uint32_t)num_samples, accumulate != 0, weight_dev, bias_dev, work_dev};
+    return done(launch_linear_map(a, dtype, ctx->sm_count, ctx->dev.status, as_stream(stream)));
 }
 
 }  // extern "C"

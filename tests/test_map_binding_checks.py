@@ -132,5 +132,5 @@ def test_c_entry_points_refuse_a_missing_context():
     assert lib.he_layer_norm(null, null, 0, 1, 1, 1, null, null, 0, 1e-5, null, 1, null, null, null) == he.HE_ERR_INVALID_ARG
     assert lib.he_layer_norm_backward(null, null, 1, null, 1, 0, 1, 1, null, null, null, 0, null, 0, null, 1, null, null, null, 0, null) == he.HE_ERR_INVALID_ARG
     assert lib.he_linear_sensitivity(null, null, 1, null, 1, 0, 1, 1, 1, null, 0, 0, null, null, null, 0, null) == he.HE_ERR_INVALID_ARG
-    assert lib.he_layer_norm_backward_work_bytes(null, 1, 1) == 0 and lib.he_linear_sensitivity_work_bytes(null, 0, 1, 1, 1) == 0
+    assert lib.he_layer_norm_backward_work_bytes(null, 1, 1) == 0 and lib.he_linear_sensitivity_work_bytes(null, 0, 1, 1, 1, 0, 0) == 0
     assert isinstance(lib, ctypes.CDLL)
