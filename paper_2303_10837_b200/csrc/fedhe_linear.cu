@@ -19,22 +19,33 @@ namespace {
 constexpr uint32_t DEPTH = 64;                          // rows of a stage
 constexpr uint32_t GROUP = 64, GROUP_BYTES = DEPTH * 128;  // columns of a swizzled group, 128 bytes of each row
 constexpr uint32_t MOST_N = 256;                        // inputs of a tile; its outputs are the 128 lanes of tensor memory of each block
-// Tensor memory adds without rounding to nearest, so that a long sum loses 2^-24 of itself for each step of 16 rows: pieces of
-// so many rows are summed there, and their sums added in fp32.
-constexpr uint32_t PIECE = 512;
+// Tensor memory adds without rounding to nearest, so that a long sum of magnitudes loses about 2^-24 of itself for each step of 16 rows (8192
+// rows in pieces of 512: 2.8e-6 off, of 128: see below).  Pieces of so many rows are summed there, and their sums added in fp32.
+// Where rows are samples of their own a piece costs no more than its epilogue; a sample's second piece waits for the first one's, so
+// those are longer, and their terms of both signs lose less.
+constexpr uint32_t PIECE = 512, PIECE_ALONE = 128;
 constexpr uint32_t THREADS = 384;                       // warps: loads, products, two between them, eight of the epilogue
 constexpr uint32_t STAGING = 128 * (MOST_N + 1) * 4;
 constexpr uint32_t TRIES = 256;                         // of 10 ms at most
 
 // ---- the hardware's instructions ----
 
+// One lane of a warp, the same each time.  Instructions of one thread stand behind this and not behind a comparison of the lane: the
+// compiler then knows that there is one, and needs no loop over threads around each (four products and their commit took 680 clocks so).
+__device__ __forceinline__ bool elected() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
 }
-// arrives at a barrier of the block `rank` of the cluster
+// Arrives at a barrier of the block `rank` of the cluster.  What it tells of was written by copies, or fenced for them and the tensor cores,
+// so no fence of the cluster's scope is asked for here (with one at each of these and of the waits: 119 us instead of 95 for 8192 x 2048 x 2048).
 __device__ __forceinline__ void bar_arrive(uint64_t *b, uint32_t rank) {
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_at(b)),
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tmbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(smem_at(b)),
                  "r"(rank)
                  : "memory");
 }
@@ -45,7 +56,7 @@ __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes) {
 __device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity) {
     for (uint32_t i = 0; i < TRIES; i++) {
         uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done)
                      : "r"(smem_at(b)), "r"(parity)
                      : "memory");
@@ -153,7 +164,7 @@ struct Pieces {
             k++;
         }
         p.row = at;
-        p.count = min((int32_t)PIECE, hi - at);
+        p.count = min((int32_t)(offsets ? PIECE : PIECE_ALONE), hi - at);
         p.first = !offsets || at == lo;
         at += p.count;
         p.last = !offsets || at == hi;
@@ -196,7 +207,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     __shared__ uint64_t full[MOST_STAGES], ready[MOST_STAGES], empty[MOST_STAGES], sum_full[2], sum_empty[2], drained;
     __shared__ uint32_t tmem_base;
     cg::cluster_group cluster = cg::this_cluster();
-    const uint32_t tid = threadIdx.x, warp = tid / 32, lane = tid & 31u;
+    const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid & 31u;
     const uint32_t rank = cluster.block_rank(), half = rank % CG, leader = rank - half, split = rank / CG;
     const uint32_t tile = blockIdx.x / (job.splits * CG);
     const uint32_t o0 = (tile / job.tiles_i) * 128 * CG + half * 128, i0 = (tile % job.tiles_i) * job.n;
@@ -246,7 +257,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                 for (int32_t r = 0; well && r < p.count; r += DEPTH) {
                     well = bar_wait(&empty[s], (turn & 1u) ^ 1u);
                     if (!well) break;
-                    if (lane == 0) {
+                    if (elected()) {
                         const uint32_t at = smem + s * stage_bytes;
                         const uint32_t sixteens = min(4u, (uint32_t)(p.count - r + 15) / 16);
                         bar_expect(&full[s], (ga + gb) * sixteens * 16 * 128);
@@ -289,7 +300,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         well = bar_wait(&ready[s], turn & 1u);
                         if (!well) break;
                         tmem_order_after();
-                        if (lane == 0) {
+                        if (elected()) {
                             const uint32_t at = smem + s * stage_bytes;
                             const uint32_t sixteens = min(4u, (uint32_t)(p.count - r + 15) / 16);
                             for (uint32_t h = 0; h < sixteens; h++) {
@@ -302,11 +313,11 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         __syncwarp();
                         if (++s == job.stages) s = 0, turn++;
                     }
-                if (lane == 0 && well) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
+                if (well && elected()) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
                 __syncwarp();
             }
             // products under way use both blocks' memory
-            if (lane == 0) commit<CG>(&drained, (uint16_t)(3u << leader));
+            if (elected()) commit<CG>(&drained, (uint16_t)(3u << leader));
             __syncwarp();
         }
         if (!bar_wait(&drained, 0)) well = false;
@@ -331,7 +342,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         }
                         __syncwarp();
-                        if (lane == 0) bar_arrive(&ready[s], leader);
+                        if (elected()) bar_arrive(&ready[s], leader);
                     }
                     if (++s == job.stages) s = 0, turn++;
                 }
@@ -378,7 +389,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
             }
             tmem_order_before();
             __syncwarp();
-            if (lane == 0) {
+            if (elected()) {
                 if (!p.first || p.last) bar_arrive(&sum_empty[b], leader);
                 if (!p.first && p.last) bar_arrive(&sum_empty[held], leader);
             }
@@ -409,11 +420,22 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     for (uint32_t o = first + warp; o < behind; o += THREADS / 32) {
         if (o0 + o >= job.outputs) break;
         float *out = job.weight + (size_t)(o0 + o) * job.inputs + i0;
-        for (uint32_t c = lane; c < width; c += 32) {
-            float v = 0.0f;
-            for (uint32_t f = 0; f < job.splits; f++) v += *cluster.map_shared_rank(sums + o * pitch + c, f * CG + half);
-            out[c] = job.accumulate ? out[c] + v : v;
+        float v[MOST_N / 32];                // a row at once: loads from other blocks take long, stores should not wait for one another
+#pragma unroll
+        for (int j = 0; j < (int)MOST_N / 32; j++) v[j] = 0.0f;
+        for (uint32_t f = 0; f < job.splits; f++) {
+            const float *from = job.splits == 1 ? sums : cluster.map_shared_rank(sums, f * CG + half);
+#pragma unroll
+            for (int j = 0; j < (int)MOST_N / 32; j++)
+                if (j * 32 < job.n) v[j] += from[o * pitch + j * 32 + lane];
         }
+        if (job.accumulate)
+#pragma unroll
+            for (int j = 0; j < (int)MOST_N / 32; j++)
+                if (j * 32 + lane < width) v[j] += out[j * 32 + lane];
+#pragma unroll
+        for (int j = 0; j < (int)MOST_N / 32; j++)
+            if (j * 32 + lane < width) out[j * 32 + lane] = v[j];
     }
     cluster.sync();                          // nobody leaves while its memory is read
 }
