@@ -16,7 +16,9 @@ namespace fedhe {
 
 namespace {
 
-constexpr uint32_t DEPTH = 64;                          // rows of a stage
+// Rows of a stage.  What a role does for a stage takes it some 400 clocks of dependent instructions, so stages are large.
+constexpr uint32_t DEPTH = 128;
+constexpr uint32_t SHORT = 32;                          // rows of a smaller copy, for the ends of samples
 constexpr uint32_t GROUP = 64, GROUP_BYTES = DEPTH * 128;  // columns of a swizzled group, 128 bytes of each row
 constexpr uint32_t MOST_N = 256;                        // inputs of a tile; its outputs are the 128 lanes of tensor memory of each block
 // Tensor memory adds without rounding to nearest, so that a long sum of magnitudes loses about 2^-24 of itself for each step of 16 rows (8192
@@ -42,6 +44,11 @@ __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
 }
+// Registers of a warpgroup's threads: the epilogue's need those that the others leave.  At the launch 168 each, 3 * 168 = 72 + 2 * 216.
+template <int N>
+__device__ __forceinline__ void registers_less() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 // Arrives at a barrier of the block `rank` of the cluster.  What it tells of was written by copies, or fenced for them and the tensor cores,
 // so no fence of the cluster's scope is asked for here (with one at each of these and of the waits: 119 us instead of 95 for 8192 x 2048 x 2048).
 __device__ __forceinline__ void bar_arrive(uint64_t *b, uint32_t rank) {
@@ -117,6 +124,12 @@ __device__ __forceinline__ void tmem_order_after() { asm volatile("tcgen05.fence
 __device__ __forceinline__ void tmem_get32(uint32_t at, float (&v)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
                  : REGS16(v, 0), REGS16(v, 16)
+                 : "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_get64(uint32_t at, float (&v)[64]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : REGS16(v, 0), REGS16(v, 16), REGS16(v, 32), REGS16(v, 48)
                  : "r"(at)
                  : "memory");
 }
@@ -199,8 +212,8 @@ __device__ __forceinline__ uint32_t piece_of_x(uint32_t pair) { return (0x010102
 // Of a cluster of splits * CG blocks, CG blocks work on a tile of CG * 128 outputs and n inputs: each holds 128 outputs' columns of dy
 // and n / CG inputs' columns of x, and the sums of its outputs.
 template <int CG>
-__global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_constant__ CUtensorMap dy64, const __grid_constant__ CUtensorMap dy16,
-                                                                const __grid_constant__ CUtensorMap x64, const __grid_constant__ CUtensorMap x16,
+__global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_constant__ CUtensorMap dy_deep, const __grid_constant__ CUtensorMap dy_short,
+                                                                const __grid_constant__ CUtensorMap x_deep, const __grid_constant__ CUtensorMap x_short,
                                                                 const LinearJob job) {
     extern __shared__ uint8_t raw[];
     constexpr uint32_t MOST_STAGES = 12;
@@ -248,7 +261,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     }
     Piece p;
     bool well = true;
-    float total[4][32];                                                        // of the epilogue's warps
+    if (warp < 4) {
+    registers_less<72>();
     if (warp == 0) {
         uint32_t s = 0, turn = 0;
         while (well && pieces.next(p))
@@ -259,18 +273,18 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                     if (!well) break;
                     if (elected()) {
                         const uint32_t at = smem + s * stage_bytes;
-                        const uint32_t sixteens = min(4u, (uint32_t)(p.count - r + 15) / 16);
-                        bar_expect(&full[s], (ga + gb) * sixteens * 16 * 128);
+                        const uint32_t shorts = min(DEPTH / SHORT, (uint32_t)(p.count - r + SHORT - 1) / SHORT);
+                        bar_expect(&full[s], (ga + gb) * shorts * SHORT * 128);
                         const int32_t row = p.row + r;
-                        if (sixteens == 4) {
-                            for (uint32_t g = 0; g < ga; g++) tma_load(at + g * GROUP_BYTES, &dy64, (int32_t)(o0 + g * GROUP), row, pa, &full[s]);
-                            for (uint32_t g = 0; g < gb; g++) tma_load(at + a_bytes + g * GROUP_BYTES, &x64, (int32_t)(ib + g * GROUP), row, pb, &full[s]);
+                        if (shorts == DEPTH / SHORT) {
+                            for (uint32_t g = 0; g < ga; g++) tma_load(at + g * GROUP_BYTES, &dy_deep, (int32_t)(o0 + g * GROUP), row, pa, &full[s]);
+                            for (uint32_t g = 0; g < gb; g++) tma_load(at + a_bytes + g * GROUP_BYTES, &x_deep, (int32_t)(ib + g * GROUP), row, pb, &full[s]);
                         } else {
-                            for (uint32_t h = 0; h < sixteens; h++) {
-                                for (uint32_t g = 0; g < ga; g++)
-                                    tma_load(at + g * GROUP_BYTES + h * 2048, &dy16, (int32_t)(o0 + g * GROUP), row + (int32_t)h * 16, pa, &full[s]);
-                                for (uint32_t g = 0; g < gb; g++)
-                                    tma_load(at + a_bytes + g * GROUP_BYTES + h * 2048, &x16, (int32_t)(ib + g * GROUP), row + (int32_t)h * 16, pb, &full[s]);
+                            for (uint32_t h = 0; h < shorts; h++) {
+                                const uint32_t to = at + h * SHORT * 128;
+                                const int32_t from = row + (int32_t)(h * SHORT);
+                                for (uint32_t g = 0; g < ga; g++) tma_load(to + g * GROUP_BYTES, &dy_short, (int32_t)(o0 + g * GROUP), from, pa, &full[s]);
+                                for (uint32_t g = 0; g < gb; g++) tma_load(to + a_bytes + g * GROUP_BYTES, &x_short, (int32_t)(ib + g * GROUP), from, pb, &full[s]);
                             }
                         }
                     }
@@ -302,10 +316,13 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         tmem_order_after();
                         if (elected()) {
                             const uint32_t at = smem + s * stage_bytes;
-                            const uint32_t sixteens = min(4u, (uint32_t)(p.count - r + 15) / 16);
-                            for (uint32_t h = 0; h < sixteens; h++) {
-                                multiply<CG>(d, operand(at + h * 2048), operand(at + a_bytes + h * 2048), job.what, add);
-                                add = true;
+                            const uint32_t sixteens = min(DEPTH / 16, (uint32_t)(p.count - r + 15) / 16);
+                            const uint64_t a = operand(at), b2 = operand(at + a_bytes);
+                            if (sixteens == DEPTH / 16) {
+#pragma unroll
+                                for (uint32_t h = 0; h < DEPTH / 16; h++) multiply<CG>(d, a + h * (2048 >> 4), b2 + h * (2048 >> 4), job.what, add || h);
+                            } else {
+                                for (uint32_t h = 0; h < sixteens; h++) multiply<CG>(d, a + h * (2048 >> 4), b2 + h * (2048 >> 4), job.what, add || h);
                             }
                             commit<CG>(&empty[s], (uint16_t)(3u << leader));
                         }
@@ -321,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
             __syncwarp();
         }
         if (!bar_wait(&drained, 0)) well = false;
-    } else if (warp < 4) {
+    } else {
         // Rows of the next sample, or none of any, that came with a sample's last ones count as zeros.  The two warps take stages in turn.
         uint32_t s = 0, turn = 0, i = 0;
         while (well && pieces.next(p))
@@ -346,78 +363,87 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                     }
                     if (++s == job.stages) s = 0, turn++;
                 }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-            for (int e = 0; e < 32; e++) total[j][e] = 0.0f;
-        const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - 4) / 4 * cols;
-        uint32_t uses[2] = {0, 0}, held = 1;
-        while (well && pieces.next(p)) {
-            if (p.first) held ^= 1;
-            const uint32_t b = p.first ? held : held ^ 1;
-            const uint32_t use = b ? uses[1]++ : uses[0]++;
-            well = bar_wait(&sum_full[b], use & 1u);
-            if (!well) break;
+    }
+        if (!well && lane == 0) atomicOr(job.status, STATUS_COPY);
+        cluster.sync();                      // every product of the pair is done, and every sum read
+        if (warp == 1) {
             tmem_order_after();
-            if (p.first && p.last) {
+            tmem_give<CG>(tmem);
+        }
+        cluster.sync();
+        cluster.sync();
+        return;
+    }
+    // the epilogue's warps: 32 lanes of tensor memory, half of a tile's columns
+    registers_more<216>();
+    float total[128];
 #pragma unroll
-                for (int j = 0; j < 4; j++)
-                    if (j * 32 < cols) {
-                        float v[32];
-                        tmem_get32(mine + b * MOST_N + j * 32, v);
+    for (int e = 0; e < 128; e++) total[e] = 0.0f;
+    const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - 4) / 4 * cols;
+    uint32_t uses[2] = {0, 0}, held = 1;
+    while (well && pieces.next(p)) {
+        if (p.first) held ^= 1;
+        const uint32_t b = p.first ? held : held ^ 1;
+        const uint32_t use = b ? uses[1]++ : uses[0]++;
+        well = bar_wait(&sum_full[b], use & 1u);
+        if (!well) break;
+        tmem_order_after();
+        const uint32_t at = mine + b * MOST_N;
+        if (p.first && p.last) {
 #pragma unroll
-                        for (int e = 0; e < 32; e++) total[j][e] += fabsf(v[e]);
-                    }
-            } else if (!p.first) {
-                // a long sample: its first piece's place holds the sum of its pieces
+            for (int j = 0; j < 128; j += 64) {
+                if (j + 64 <= cols) {
+                    float v[64];
+                    tmem_get64(at + j, v);
 #pragma unroll
-                for (int j = 0; j < 8; j++)
-                    if (j * 16 < cols) {
-                        float v[16], u[16];
-                        tmem_get16(mine + b * MOST_N + j * 16, v);
-                        tmem_get16(mine + held * MOST_N + j * 16, u);
+                    for (int e = 0; e < 64; e++) total[j + e] += fabsf(v[e]);
+                } else if (j < cols) {
+                    float v[32];
+                    tmem_get32(at + j, v);
 #pragma unroll
-                        for (int e = 0; e < 16; e++) u[e] += v[e];
-                        if (p.last) {
-#pragma unroll
-                            for (int e = 0; e < 16; e++) total[j / 2][j % 2 * 16 + e] += fabsf(u[e]);
-                        } else {
-                            tmem_put16(mine + held * MOST_N + j * 16, u);
-                        }
-                    }
+                    for (int e = 0; e < 32; e++) total[j + e] += fabsf(v[e]);
+                }
             }
-            tmem_order_before();
-            __syncwarp();
-            if (elected()) {
-                if (!p.first || p.last) bar_arrive(&sum_empty[b], leader);
-                if (!p.first && p.last) bar_arrive(&sum_empty[held], leader);
-            }
+        } else if (!p.first) {
+            // a long sample: its first piece's place holds the sum of its pieces
+#pragma unroll
+            for (int j = 0; j < 128; j += 16)
+                if (j < cols) {
+                    float v[16], u[16];
+                    tmem_get16(at + j, v);
+                    tmem_get16(mine + held * MOST_N + j, u);
+#pragma unroll
+                    for (int e = 0; e < 16; e++) u[e] += v[e];
+                    if (p.last) {
+#pragma unroll
+                        for (int e = 0; e < 16; e++) total[j + e] += fabsf(u[e]);
+                    } else {
+                        tmem_put16(mine + held * MOST_N + j, u);
+                    }
+                }
+        }
+        tmem_order_before();
+        __syncwarp();
+        if (elected()) {
+            if (!p.first || p.last) bar_arrive(&sum_empty[b], leader);
+            if (!p.first && p.last) bar_arrive(&sum_empty[held], leader);
         }
     }
     if (!well && lane == 0) atomicOr(job.status, STATUS_COPY);
-    // every product of the pair is done: the stages' memory takes the sums
-    __syncthreads();
-    cluster.sync();
-    if (warp == 1) {
-        tmem_order_after();
-        tmem_give<CG>(tmem);
-    }
+    cluster.sync();                          // every product of the pair is done: the stages' memory takes the sums
     float *sums = reinterpret_cast<float *>(raw + (smem - smem_at(raw)));
     const uint32_t pitch = job.n + 1;
-    if (warp >= 4) {
-        float *to = sums + ((warp & 3u) * 32 + lane) * pitch + (warp - 4) / 4 * (job.n / 2);
+    float *to = sums + ((warp & 3u) * 32 + lane) * pitch + (warp - 4) / 4 * cols;
 #pragma unroll
-        for (int j = 0; j < 4; j++)
-            if (j * 32 < job.n / 2)
+    for (int j = 0; j < 128; j += 32)
+        if (j < cols)
 #pragma unroll
-                for (int e = 0; e < 32; e++) to[j * 32 + e] = total[j][e];
-    }
+            for (int e = 0; e < 32; e++) to[j + e] = total[j + e];
     cluster.sync();
     // the splits' sums, each block some outputs of its 128
     const uint32_t first = 128 * split / job.splits, behind = 128 * (split + 1) / job.splits;
     const uint32_t width = min(job.n, job.inputs - i0);
-    for (uint32_t o = first + warp; o < behind; o += THREADS / 32) {
+    for (uint32_t o = first + warp - 4; o < behind; o += 8) {
         if (o0 + o >= job.outputs) break;
         float *out = job.weight + (size_t)(o0 + o) * job.inputs + i0;
         float v[MOST_N / 32];                // a row at once: loads from other blocks take long, stores should not wait for one another
@@ -524,7 +550,7 @@ Plan plan_of(const LinearMapArgs &a, uint32_t pairs, int n_sm) {
     for (uint32_t cg = 1; cg <= 2; cg++)
         for (uint32_t n = 64 * cg; n <= MOST_N; n += 64 * cg)
             for (uint32_t c = 1; c * cg <= 8; c++) {
-                if (c > 1 && c > (a.over == SumOver::SAMPLES ? (size_t)a.samples : (a.rows + DEPTH - 1) / DEPTH)) break;
+                if (c > 1 && c > (a.over == SumOver::SAMPLES ? (size_t)a.samples : (a.rows + PIECE_ALONE - 1) / PIECE_ALONE)) break;
                 const double tiles = (double)((a.outputs + 128 * cg - 1) / (128 * cg)) * (double)((a.inputs + n - 1) / n);
                 const double waves = ceil(tiles * cg * c / n_sm);
                 // clocks of a row: its products, or its bytes at what L2 gives an SM
@@ -597,8 +623,8 @@ cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *
     const Plan plan = plan_of(a, pairs, n_sm);
     CUtensorMap m[4];
     const bool half = dtype == HE_F16;
-    if (!tensor_map(m[0], dy.p, a.outputs, a.rows, dy.stride, parts, half, 64) || !tensor_map(m[1], dy.p, a.outputs, a.rows, dy.stride, parts, half, 16) ||
-        !tensor_map(m[2], x.p, a.inputs, a.rows, x.stride, parts, half, 64) || !tensor_map(m[3], x.p, a.inputs, a.rows, x.stride, parts, half, 16))
+    if (!tensor_map(m[0], dy.p, a.outputs, a.rows, dy.stride, parts, half, DEPTH) || !tensor_map(m[1], dy.p, a.outputs, a.rows, dy.stride, parts, half, SHORT) ||
+        !tensor_map(m[2], x.p, a.inputs, a.rows, x.stride, parts, half, DEPTH) || !tensor_map(m[3], x.p, a.inputs, a.rows, x.stride, parts, half, SHORT))
         return cudaErrorInvalidValue;
     const uint32_t stage = 2 * GROUP_BYTES + (plan.n / plan.cg + GROUP - 1) / GROUP * GROUP_BYTES;
     LinearJob job{};
