@@ -26,7 +26,7 @@ constexpr uint32_t MOST_N = 256;                        // inputs of a tile; its
 // Where rows are samples of their own a piece costs no more than its epilogue; a sample's second piece waits for the first one's, so
 // those are longer, and their terms of both signs lose less.
 constexpr uint32_t PIECE = 512, PIECE_ALONE = 128;
-constexpr uint32_t THREADS = 384;                       // warps: loads, products, two between them, eight of the epilogue
+constexpr uint32_t THREADS = 384;                       // warps: copies of dy, products, copies of x, what is between them, eight of the epilogue
 constexpr uint32_t STAGING = 128 * (MOST_N + 1) * 4;
 constexpr uint32_t TRIES = 256;                         // of 10 ms at most
 
@@ -44,6 +44,7 @@ __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__
 __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
 }
+__device__ __forceinline__ void block_meets() { asm volatile("barrier.sync 1, %0;" ::"n"(THREADS) : "memory"); }
 // Registers of a warpgroup's threads: the epilogue's need those that the others leave.  At the launch 168 each, 3 * 168 = 72 + 2 * 216.
 template <int N>
 __device__ __forceinline__ void registers_less() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -147,43 +148,79 @@ __device__ __forceinline__ void tmem_put16(uint32_t at, const float (&v)[16]) {
 }
 #undef REGS16
 
-// ---- what every role of a block goes through: the pieces of its samples ----
+// ---- what every role of a block goes through: the stages of its samples, listed in shared memory ----
 
-struct Piece {
-    int32_t row, count;      // count > 0
-    bool first, last;        // of a sample
+struct Stage {
+    int32_t row;
+    uint32_t what;           // rows (1 .. DEPTH), flags, and from PAIR on which pieces of fp32 values
+    static constexpr uint32_t ROWS = 0xff, BEGINS = 1u << 8, ENDS = 1u << 9;           // a piece
+    static constexpr uint32_t FIRST = 1u << 10, LAST = 1u << 11, PAIR = 12;            // piece of its sample
 };
+constexpr uint32_t LISTED = 1024;
 
-// By a whole warp; `offsets` null: the rows [lo, hi) by themselves, where any cut will do.
-struct Pieces {
-    const int32_t *offsets;
-    uint32_t k, end, base;
-    int32_t rows, held, lo, hi, at;
-    __device__ __forceinline__ int32_t offset(uint32_t i) {
-        if (i - base >= 32u) {
-            base = i;
-            const uint32_t j = min(i + (threadIdx.x & 31u), end);
-            held = __ldg(offsets + j);
-        }
-        const int32_t v = __shfl_sync(0xffffffffu, held, i - base);
-        return min(max(v, 0), rows);
-    }
-    __device__ __forceinline__ bool next(Piece &p) {
-        while (at >= hi) {
-            if (!offsets || k >= end) return false;
-            lo = offset(k);
-            hi = offset(k + 1);
-            at = lo;
-            k++;
-        }
-        p.row = at;
-        p.count = min((int32_t)(offsets ? PIECE : PIECE_ALONE), hi - at);
-        p.first = !offsets || at == lo;
-        at += p.count;
-        p.last = !offsets || at == hi;
-        return true;
-    }
+// Where the list goes on: entry `at` of sample k.
+struct Cursor {
+    uint32_t k, end;         // samples
+    uint32_t at;
+    int32_t lo, hi;          // the rows of a block whose rows are samples of their own
 };
+// Entries of a sample of `count` rows in pieces of `piece` rows, each `pairs` times over.
+__device__ __forceinline__ uint32_t entries_of(uint32_t count, uint32_t piece, uint32_t pairs) {
+    const uint32_t whole = count / piece;
+    return (whole * (piece / DEPTH) + (count % piece + DEPTH - 1) / DEPTH) * pairs;
+}
+__device__ __forceinline__ Stage entry_of(int32_t row, uint32_t count, uint32_t piece, uint32_t pairs, uint32_t j, bool alone) {
+    const uint32_t per = piece / DEPTH * pairs, n = j / per, in = j % per, behind = n * piece;
+    const uint32_t rows = min(piece, count - behind), stages = (rows + DEPTH - 1) / DEPTH, pair = in / stages, c = in % stages;
+    uint32_t what = min(DEPTH, rows - c * DEPTH) | pair << Stage::PAIR;
+    if (in == 0) what |= Stage::BEGINS;
+    if (in + 1 == stages * pairs) what |= Stage::ENDS;
+    if (alone || behind == 0) what |= Stage::FIRST;
+    if (alone || behind + rows == count) what |= Stage::LAST;
+    return Stage{row + (int32_t)(behind + c * DEPTH), what};
+}
+// The next entries, at most LISTED; by a warp.  What the offsets say is brought within the rows.
+__device__ __forceinline__ uint32_t list_stages(Stage *list, Cursor &c, const int32_t *offsets, int32_t rows, uint32_t pairs) {
+    const uint32_t lane = threadIdx.x & 31u;
+    uint32_t n = 0;
+    if (!offsets) {
+        const uint32_t count = (uint32_t)(c.hi - c.lo), all = entries_of(count, PIECE_ALONE, pairs);
+        n = min(LISTED, all - c.at);
+        for (uint32_t i = lane; i < n; i += 32) list[i] = entry_of(c.lo, count, PIECE_ALONE, pairs, c.at + i, true);
+        c.at += n;
+        return n;
+    }
+    while (c.k < c.end && n < LISTED) {
+        const uint32_t k = c.k + lane;
+        int32_t lo = 0, count = 0;
+        if (k < c.end) {
+            lo = min(max(__ldg(offsets + k), 0), rows);
+            count = min(max(__ldg(offsets + k + 1), lo), rows) - lo;
+        }
+        const uint32_t skip = lane == 0 ? c.at : 0, mine = entries_of((uint32_t)count, PIECE, pairs) - skip;
+        uint32_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= (uint32_t)o) upto += v;
+        }
+        const uint32_t from = n + upto - mine, fit = from >= LISTED ? 0 : min(mine, LISTED - from);
+        for (uint32_t i = 0; i < fit; i++) list[from + i] = entry_of(lo, (uint32_t)count, PIECE, pairs, skip + i, false);
+        // the first sample that did not fit whole
+        const uint32_t cut = __ballot_sync(0xffffffffu, fit < mine);
+        const uint32_t total = __shfl_sync(0xffffffffu, upto, 31);
+        if (cut) {
+            const uint32_t who = __ffs(cut) - 1;
+            c.at = __shfl_sync(0xffffffffu, skip + fit, who);
+            c.k += who;
+            return LISTED;
+        }
+        n += total;
+        c.k = min(c.k + 32, c.end);
+        c.at = 0;
+    }
+    return n;
+}
 // the first offset that is not below a row
 __device__ __forceinline__ uint32_t first_at(const int32_t *offsets, uint32_t count, int64_t row) {
     uint32_t lo = 0, hi = count;
@@ -218,7 +255,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     extern __shared__ uint8_t raw[];
     constexpr uint32_t MOST_STAGES = 12;
     __shared__ uint64_t full[MOST_STAGES], ready[MOST_STAGES], empty[MOST_STAGES], sum_full[2], sum_empty[2], drained;
-    __shared__ uint32_t tmem_base;
+    __shared__ uint32_t tmem_base, listed;
+    __shared__ alignas(8) Stage list[LISTED];
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid & 31u;
     const uint32_t rank = cluster.block_rank(), half = rank % CG, leader = rank - half, split = rank / CG;
@@ -232,7 +270,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     const uint32_t a_bytes = 2 * GROUP_BYTES, stage_bytes = a_bytes + (nb + GROUP - 1) / GROUP * GROUP_BYTES;
     if (tid == 0) {
         for (uint32_t s = 0; s < job.stages; s++) {
-            bar_init(&full[s], 1);
+            bar_init(&full[s], 2);
             bar_init(&ready[s], CG);
             bar_init(&empty[s], 1);
         }
@@ -249,121 +287,128 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     tmem_order_after();
     const uint32_t tmem = tmem_base;
 
-    Pieces pieces{job.offsets, 0, 0, 0x80000000u, (int32_t)job.rows, 0, 0, 0, 0};
+    Cursor next{0, 0, 0, 0, 0};
     const int64_t r0 = (int64_t)job.rows * split / job.splits, r1 = (int64_t)job.rows * (split + 1) / job.splits;
-    if (job.offsets) {
-        // a sample goes to the split in whose share of the rows it begins
-        pieces.k = split == 0 ? 0 : first_at(job.offsets, job.samples, r0);
-        pieces.end = split + 1 == job.splits ? job.samples : first_at(job.offsets, job.samples, r1);
-    } else {
-        pieces.lo = pieces.at = (int32_t)r0;
-        pieces.hi = (int32_t)r1;
+    if (warp == 3) {
+        if (job.offsets) {
+            // a sample goes to the split in whose share of the rows it begins
+            next.k = split == 0 ? 0 : first_at(job.offsets, job.samples, r0);
+            next.end = split + 1 == job.splits ? job.samples : first_at(job.offsets, job.samples, r1);
+        } else {
+            next.lo = (int32_t)r0;
+            next.hi = (int32_t)r1;
+        }
     }
-    Piece p;
     bool well = true;
     if (warp < 4) {
-    registers_less<72>();
-    if (warp == 0) {
-        uint32_t s = 0, turn = 0;
-        while (well && pieces.next(p))
-            for (uint32_t q = 0; well && q < job.pairs; q++) {
-                const int32_t pa = job.pairs == 1 ? 0 : (int32_t)piece_of_dy(q), pb = job.pairs == 1 ? 0 : (int32_t)piece_of_x(q);
-                for (int32_t r = 0; well && r < p.count; r += DEPTH) {
-                    well = bar_wait(&empty[s], (turn & 1u) ^ 1u);
-                    if (!well) break;
+        registers_less<72>();
+        uint32_t s = 0, turn = 0, uses[2] = {0, 0}, held = 1, b = 0;
+        for (;;) {
+            if (warp == 3) {
+                const uint32_t n = list_stages(list, next, job.offsets, (int32_t)job.rows, job.pairs);
+                if (lane == 0) listed = n;
+            }
+            block_meets();
+            const uint32_t n = listed;
+            if (n == 0) break;
+            if (warp == 0 || warp == 2) {
+                // copies of dy, and of x
+                const bool of_dy = warp == 0;
+                const uint32_t groups = of_dy ? ga : gb, shift = of_dy ? 0 : a_bytes;
+                const int32_t col = (int32_t)(of_dy ? o0 : ib);
+                const CUtensorMap *deep = of_dy ? &dy_deep : &x_deep, *brief = of_dy ? &dy_short : &x_short;
+                for (uint32_t i = 0; well && i < n; i++) {
+                    const Stage e = list[i];
+                    const uint32_t shorts = ((e.what & Stage::ROWS) + SHORT - 1) / SHORT, pair = e.what >> Stage::PAIR;
+                    const int32_t part = job.pairs == 1 ? 0 : (int32_t)(of_dy ? piece_of_dy(pair) : piece_of_x(pair));
+                    const uint32_t at = smem + s * stage_bytes + shift;
+                    if (!bar_wait(&empty[s], (turn & 1u) ^ 1u)) {
+                        well = false;
+                        break;
+                    }
                     if (elected()) {
-                        const uint32_t at = smem + s * stage_bytes;
-                        const uint32_t shorts = min(DEPTH / SHORT, (uint32_t)(p.count - r + SHORT - 1) / SHORT);
-                        bar_expect(&full[s], (ga + gb) * shorts * SHORT * 128);
-                        const int32_t row = p.row + r;
-                        if (shorts == DEPTH / SHORT) {
-                            for (uint32_t g = 0; g < ga; g++) tma_load(at + g * GROUP_BYTES, &dy_deep, (int32_t)(o0 + g * GROUP), row, pa, &full[s]);
-                            for (uint32_t g = 0; g < gb; g++) tma_load(at + a_bytes + g * GROUP_BYTES, &x_deep, (int32_t)(ib + g * GROUP), row, pb, &full[s]);
-                        } else {
-                            for (uint32_t h = 0; h < shorts; h++) {
-                                const uint32_t to = at + h * SHORT * 128;
-                                const int32_t from = row + (int32_t)(h * SHORT);
-                                for (uint32_t g = 0; g < ga; g++) tma_load(to + g * GROUP_BYTES, &dy_short, (int32_t)(o0 + g * GROUP), from, pa, &full[s]);
-                                for (uint32_t g = 0; g < gb; g++) tma_load(to + a_bytes + g * GROUP_BYTES, &x_short, (int32_t)(ib + g * GROUP), from, pb, &full[s]);
-                            }
-                        }
+                        bar_expect(&full[s], groups * shorts * SHORT * 128);
+                        if (shorts == DEPTH / SHORT)
+                            for (uint32_t g = 0; g < groups; g++) tma_load(at + g * GROUP_BYTES, deep, col + (int32_t)(g * GROUP), e.row, part, &full[s]);
+                        else
+                            for (uint32_t h = 0; h < shorts; h++)
+                                for (uint32_t g = 0; g < groups; g++)
+                                    tma_load(at + g * GROUP_BYTES + h * SHORT * 128, brief, col + (int32_t)(g * GROUP), e.row + (int32_t)(h * SHORT), part, &full[s]);
                     }
                     __syncwarp();
                     if (++s == job.stages) s = 0, turn++;
                 }
-            }
-        // no copy is under way when the block ends: the last of each stage is waited for, whatever happened
-        for (uint32_t i = 0; i < job.stages; i++)
-            if (turn || i < s) {
-                const uint32_t last = i < s ? turn : turn - 1;
-                if (!bar_wait(&full[i], last & 1u)) well = false;
-            }
-    } else if (warp == 1) {
-        if (half == 0) {
-            uint32_t s = 0, turn = 0, uses[2] = {0, 0}, held = 1;
-            while (well && pieces.next(p)) {
-                if (p.first) held ^= 1;
-                const uint32_t b = p.first ? held : held ^ 1;
-                const uint32_t use = b ? uses[1]++ : uses[0]++;
-                well = bar_wait(&sum_empty[b], (use & 1u) ^ 1u);
-                tmem_order_after();
-                const uint32_t d = tmem + b * MOST_N;
-                bool add = false;
-                for (uint32_t q = 0; well && q < job.pairs; q++)
-                    for (int32_t r = 0; well && r < p.count; r += DEPTH) {
-                        well = bar_wait(&ready[s], turn & 1u);
-                        if (!well) break;
+            } else if (warp == 1) {
+                if (half == 0)
+                    for (uint32_t i = 0; well && i < n; i++) {
+                        const Stage e = list[i];
+                        const uint32_t at = smem + s * stage_bytes, sixteens = ((e.what & Stage::ROWS) + 15) / 16;
+                        if (e.what & Stage::BEGINS) {
+                            if (e.what & Stage::FIRST) held ^= 1;
+                            b = e.what & Stage::FIRST ? held : held ^ 1;
+                            const uint32_t use = b ? uses[1]++ : uses[0]++;
+                            if (!bar_wait(&sum_empty[b], (use & 1u) ^ 1u)) well = false;
+                        }
+                        if (!well || !bar_wait(&ready[s], turn & 1u)) {
+                            well = false;
+                            break;
+                        }
                         tmem_order_after();
                         if (elected()) {
-                            const uint32_t at = smem + s * stage_bytes;
-                            const uint32_t sixteens = min(DEPTH / 16, (uint32_t)(p.count - r + 15) / 16);
-                            const uint64_t a = operand(at), b2 = operand(at + a_bytes);
+                            const uint32_t d = tmem + b * MOST_N;
+                            const uint64_t oa = operand(at), ob = operand(at + a_bytes);
+                            const bool add = !(e.what & Stage::BEGINS);
                             if (sixteens == DEPTH / 16) {
 #pragma unroll
-                                for (uint32_t h = 0; h < DEPTH / 16; h++) multiply<CG>(d, a + h * (2048 >> 4), b2 + h * (2048 >> 4), job.what, add || h);
+                                for (uint32_t h = 0; h < DEPTH / 16; h++) multiply<CG>(d, oa + h * (2048 >> 4), ob + h * (2048 >> 4), job.what, add || h);
                             } else {
-                                for (uint32_t h = 0; h < sixteens; h++) multiply<CG>(d, a + h * (2048 >> 4), b2 + h * (2048 >> 4), job.what, add || h);
+                                for (uint32_t h = 0; h < sixteens; h++) multiply<CG>(d, oa + h * (2048 >> 4), ob + h * (2048 >> 4), job.what, add || h);
                             }
                             commit<CG>(&empty[s], (uint16_t)(3u << leader));
+                            if (e.what & Stage::ENDS) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
                         }
-                        add = true;
                         __syncwarp();
                         if (++s == job.stages) s = 0, turn++;
                     }
-                if (well && elected()) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
-                __syncwarp();
-            }
-            // products under way use both blocks' memory
-            if (elected()) commit<CG>(&drained, (uint16_t)(3u << leader));
-            __syncwarp();
-        }
-        if (!bar_wait(&drained, 0)) well = false;
-    } else {
-        // Rows of the next sample, or none of any, that came with a sample's last ones count as zeros.  The two warps take stages in turn.
-        uint32_t s = 0, turn = 0, i = 0;
-        while (well && pieces.next(p))
-            for (uint32_t q = 0; well && q < job.pairs; q++)
-                for (int32_t r = 0; well && r < p.count; r += DEPTH, i++) {
-                    if ((i & 1u) == warp - 2) {
-                        well = bar_wait(&full[s], turn & 1u);
-                        if (!well) break;
-                        const uint32_t left = (uint32_t)min((int32_t)DEPTH, p.count - r);
-                        if (left & 15u) {
-                            const uint32_t at = smem + s * stage_bytes + left * 128, words = (16 - (left & 15u)) * 8;
-                            for (uint32_t w = lane; w < words; w += 32) {
-                                for (uint32_t g = 0; g < ga; g++)
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
-                                for (uint32_t g = 0; g < gb; g++)
-                                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + a_bytes + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
-                            }
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                        }
-                        __syncwarp();
-                        if (elected()) bar_arrive(&ready[s], leader);
+            } else {
+                // Rows of the next sample, or none of any, that came with a sample's last ones count as zeros.
+                for (uint32_t i = 0; well && i < n; i++) {
+                    const uint32_t left = list[i].what & Stage::ROWS;
+                    if (!bar_wait(&full[s], turn & 1u)) {
+                        well = false;
+                        break;
                     }
+                    if (left & 15u) {
+                        const uint32_t at = smem + s * stage_bytes + left * 128, words = (16 - (left & 15u)) * 8;
+                        for (uint32_t w = lane; w < words; w += 32) {
+                            for (uint32_t g = 0; g < ga; g++)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
+                            for (uint32_t g = 0; g < gb; g++)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + a_bytes + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    }
+                    __syncwarp();
+                    if (elected()) bar_arrive(&ready[s], leader);
+                    __syncwarp();
                     if (++s == job.stages) s = 0, turn++;
                 }
-    }
+            }
+            block_meets();
+        }
+        if (warp == 0 || warp == 2) {
+            // no copy is under way when the block ends: the last of each stage is waited for, whatever happened
+            for (uint32_t i = 0; i < job.stages; i++)
+                if (turn || i < s) {
+                    const uint32_t last = i < s ? turn : turn - 1;
+                    if (!bar_wait(&full[i], last & 1u)) well = false;
+                }
+        } else if (warp == 1) {
+            // products under way use both blocks' memory
+            if (half == 0 && elected()) commit<CG>(&drained, (uint16_t)(3u << leader));
+            __syncwarp();
+            if (!bar_wait(&drained, 0)) well = false;
+        }
         if (!well && lane == 0) atomicOr(job.status, STATUS_COPY);
         cluster.sync();                      // every product of the pair is done, and every sum read
         if (warp == 1) {
@@ -381,53 +426,64 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     for (int e = 0; e < 128; e++) total[e] = 0.0f;
     const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - 4) / 4 * cols;
     uint32_t uses[2] = {0, 0}, held = 1;
-    while (well && pieces.next(p)) {
-        if (p.first) held ^= 1;
-        const uint32_t b = p.first ? held : held ^ 1;
-        const uint32_t use = b ? uses[1]++ : uses[0]++;
-        well = bar_wait(&sum_full[b], use & 1u);
-        if (!well) break;
-        tmem_order_after();
-        const uint32_t at = mine + b * MOST_N;
-        if (p.first && p.last) {
-#pragma unroll
-            for (int j = 0; j < 128; j += 64) {
-                if (j + 64 <= cols) {
-                    float v[64];
-                    tmem_get64(at + j, v);
-#pragma unroll
-                    for (int e = 0; e < 64; e++) total[j + e] += fabsf(v[e]);
-                } else if (j < cols) {
-                    float v[32];
-                    tmem_get32(at + j, v);
-#pragma unroll
-                    for (int e = 0; e < 32; e++) total[j + e] += fabsf(v[e]);
-                }
+    for (;;) {
+        block_meets();
+        const uint32_t n = listed;
+        if (n == 0) break;
+        for (uint32_t i = 0; well && i < n; i++) {
+            const uint32_t what = list[i].what;
+            if (!(what & Stage::ENDS)) continue;
+            const bool first = what & Stage::FIRST, last = what & Stage::LAST;
+            if (first) held ^= 1;
+            const uint32_t b = first ? held : held ^ 1;
+            const uint32_t use = b ? uses[1]++ : uses[0]++;
+            if (!bar_wait(&sum_full[b], use & 1u)) {
+                well = false;
+                break;
             }
-        } else if (!p.first) {
-            // a long sample: its first piece's place holds the sum of its pieces
+            tmem_order_after();
+            const uint32_t at = mine + b * MOST_N;
+            if (first && last) {
 #pragma unroll
-            for (int j = 0; j < 128; j += 16)
-                if (j < cols) {
-                    float v[16], u[16];
-                    tmem_get16(at + j, v);
-                    tmem_get16(mine + held * MOST_N + j, u);
+                for (int j = 0; j < 128; j += 64) {
+                    if (j + 64 <= cols) {
+                        float v[64];
+                        tmem_get64(at + j, v);
 #pragma unroll
-                    for (int e = 0; e < 16; e++) u[e] += v[e];
-                    if (p.last) {
+                        for (int e = 0; e < 64; e++) total[j + e] += fabsf(v[e]);
+                    } else if (j < cols) {
+                        float v[32];
+                        tmem_get32(at + j, v);
 #pragma unroll
-                        for (int e = 0; e < 16; e++) total[j + e] += fabsf(u[e]);
-                    } else {
-                        tmem_put16(mine + held * MOST_N + j, u);
+                        for (int e = 0; e < 32; e++) total[j + e] += fabsf(v[e]);
                     }
                 }
+            } else if (!first) {
+                // a long sample: its first piece's place holds the sum of its pieces
+#pragma unroll
+                for (int j = 0; j < 128; j += 16)
+                    if (j < cols) {
+                        float v[16], u[16];
+                        tmem_get16(at + j, v);
+                        tmem_get16(mine + held * MOST_N + j, u);
+#pragma unroll
+                        for (int e = 0; e < 16; e++) u[e] += v[e];
+                        if (last) {
+#pragma unroll
+                            for (int e = 0; e < 16; e++) total[j + e] += fabsf(u[e]);
+                        } else {
+                            tmem_put16(mine + held * MOST_N + j, u);
+                        }
+                    }
+            }
+            tmem_order_before();
+            __syncwarp();
+            if (elected()) {
+                if (!first || last) bar_arrive(&sum_empty[b], leader);
+                if (!first && last) bar_arrive(&sum_empty[held], leader);
+            }
         }
-        tmem_order_before();
-        __syncwarp();
-        if (elected()) {
-            if (!p.first || p.last) bar_arrive(&sum_empty[b], leader);
-            if (!p.first && p.last) bar_arrive(&sum_empty[held], leader);
-        }
+        block_meets();
     }
     if (!well && lane == 0) atomicOr(job.status, STATUS_COPY);
     cluster.sync();                          // every product of the pair is done: the stages' memory takes the sums
