@@ -16,17 +16,26 @@ namespace fedhe {
 
 namespace {
 
-// Rows of a stage.  What a role does for a stage takes it some 400 clocks of dependent instructions, so stages are large.
+// Rows of a stage, at most.  What a role does for a stage takes it some 600 clocks of dependent instructions, so stages are large.
 constexpr uint32_t DEPTH = 128;
-constexpr uint32_t SHORT = 32;                          // rows of a smaller copy, for the ends of samples
-constexpr uint32_t GROUP = 64, GROUP_BYTES = DEPTH * 128;  // columns of a swizzled group, 128 bytes of each row
+constexpr uint32_t GROUP = 64;                          // columns of a swizzled group: 128 bytes of each row
+constexpr uint32_t SLOTS = 16;                          // stages under way, at most
+constexpr uint32_t RING_BYTES = 196608;
+// Boxes of a copy have 128, 64, 32 or 16 rows: a stage is copied in as many as its rows have bits, no further than the next sixteen.
+constexpr int BOXES = 4;
+struct Maps {
+    CUtensorMap dy[BOXES], x[BOXES];
+};
 constexpr uint32_t MOST_N = 256;                        // inputs of a tile; its outputs are the 128 lanes of tensor memory of each block
 // Tensor memory adds without rounding to nearest, so that a long sum of magnitudes loses about 2^-24 of itself for each step of 16 rows (8192
 // rows in pieces of 512: 2.8e-6 off, of 128: see below).  Pieces of so many rows are summed there, and their sums added in fp32.
 // Where rows are samples of their own a piece costs no more than its epilogue; a sample's second piece waits for the first one's, so
 // those are longer, and their terms of both signs lose less.
 constexpr uint32_t PIECE = 512, PIECE_ALONE = 128;
-constexpr uint32_t THREADS = 384;                       // warps: copies of dy, products, copies of x, what is between them, eight of the epilogue
+// Warps by role: a stage's way through any of them takes some hundred clocks that nothing hides, so the work between copies and products
+// is spread over eight.
+constexpr uint32_t COPIES = 4, PRODUCTS = 4, PLACES = 5, TAILS = 6, EPILOGUE = 8;      // TAILS: two warps
+constexpr uint32_t THREADS = 512;
 constexpr uint32_t STAGING = 128 * (MOST_N + 1) * 4;
 constexpr uint32_t TRIES = 256;                         // of 10 ms at most
 
@@ -45,7 +54,7 @@ __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_at(b)), "r"(count) : "memory");
 }
 __device__ __forceinline__ void block_meets() { asm volatile("barrier.sync 1, %0;" ::"n"(THREADS) : "memory"); }
-// Registers of a warpgroup's threads: the epilogue's need those that the others leave.  At the launch 168 each, 3 * 168 = 72 + 2 * 216.
+// Registers of a warpgroup's threads: the epilogue's need those that the others leave.  At the launch 128 each, 4 * 128 = 2 * 48 + 2 * 208.
 template <int N>
 __device__ __forceinline__ void registers_less() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -62,25 +71,38 @@ __device__ __forceinline__ void bar_expect(uint64_t *b, uint32_t bytes) {
 }
 // By a whole warp; false after TRIES: something that should have come did not.
 __device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity) {
+    const uint32_t at = smem_at(b);
     for (uint32_t i = 0; i < TRIES; i++) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done)
-                     : "r"(smem_at(b)), "r"(parity)
+                     : "r"(at), "r"(parity)
                      : "memory");
         if (__all_sync(0xffffffffu, done)) return true;
     }
     return false;
 }
-__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, int32_t col, int32_t row, int32_t part, uint64_t *bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to), "l"(map),
-                 "r"(col), "r"(row), "r"(part), "r"(smem_at(bar))
-                 : "memory");
+// Copies a box to this block's shared memory; with CG = 2 the barrier may be the pair's other block's.
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, int32_t col, int32_t row, int32_t part, uint32_t bar) {
+    if (CG == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to), "l"(map),
+                     "r"(col), "r"(row), "r"(part), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to), "l"(map),
+                     "r"(col), "r"(row), "r"(part), "r"(bar)
+                     : "memory");
 }
-// An operand in shared memory whose rows (the contracted index) are 128 bytes of a group of 64 columns, swizzled in atoms of eight rows: groups
-// are GROUP_BYTES apart, atoms 1024.
-__device__ __forceinline__ uint64_t operand(uint32_t at) {
-    return (uint64_t)((at >> 4) & 0x3fff) | (uint64_t)(GROUP_BYTES >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+__device__ __forceinline__ uint32_t mapped(uint32_t at, uint32_t rank) {      // to the block `rank` of the cluster
+    uint32_t there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    return there;
+}
+// An operand in shared memory whose rows (the contracted index) are 128 bytes of a group of 64 columns, swizzled in atoms of eight rows, which
+// are 1024 bytes apart; groups are `ring` rows apart.
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t ring) {
+    return (uint64_t)((at >> 4) & 0x3fff) | (uint64_t)(ring * 8) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 template <int CG>
 __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t what, bool add) {
@@ -236,7 +258,7 @@ struct LinearJob {
     const int32_t *offsets;
     uint32_t samples, rows, inputs, outputs;
     uint32_t n, splits, tiles_i;      // inputs of a tile; blocks (or pairs) that share a tile's samples
-    uint32_t stages, pairs, what;     // products of pieces of fp32 operands: 6, or 1; the instruction's descriptor
+    uint32_t ring, pairs, what;       // rows that shared memory holds; products of pieces of fp32 operands: 6, or 1; the instruction's descriptor
     bool accumulate;
     float *weight;
     int *status;
@@ -248,15 +270,16 @@ __device__ __forceinline__ uint32_t piece_of_x(uint32_t pair) { return (0x010102
 
 // Of a cluster of splits * CG blocks, CG blocks work on a tile of CG * 128 outputs and n inputs: each holds 128 outputs' columns of dy
 // and n / CG inputs' columns of x, and the sums of its outputs.
+// Rows go through shared memory in a ring, in which a stage takes as many as it has, rounded up to 16.
 template <int CG>
-__global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_constant__ CUtensorMap dy_deep, const __grid_constant__ CUtensorMap dy_short,
-                                                                const __grid_constant__ CUtensorMap x_deep, const __grid_constant__ CUtensorMap x_short,
-                                                                const LinearJob job) {
+__global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_constant__ Maps maps, const LinearJob job) {
     extern __shared__ uint8_t raw[];
-    constexpr uint32_t MOST_STAGES = 12;
-    __shared__ uint64_t full[MOST_STAGES], ready[MOST_STAGES], empty[MOST_STAGES], sum_full[2], sum_empty[2], drained;
+    // A stage is full, in the block that issues the products, when that block's copying warps have arrived with what they and the other block's
+    // copy, when there is a place for its sum, and when each block has cleared what came with a sample's last rows; `part`: the block's copies
+    // of those.
+    __shared__ uint64_t full[SLOTS], part[SLOTS], empty[SLOTS], sum_full[2], sum_empty[2], drained;
     __shared__ uint32_t tmem_base, listed;
-    __shared__ alignas(8) Stage list[LISTED];
+    __shared__ alignas(8) Stage list[LISTED + 1];
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid / 32, 0), lane = tid & 31u;
     const uint32_t rank = cluster.block_rank(), half = rank % CG, leader = rank - half, split = rank / CG;
@@ -266,12 +289,17 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     // groups of 64 columns that hold anything; what multiplies the others lies outside the result
     const uint32_t ga = o0 >= job.outputs ? 0 : min(2u, (job.outputs - o0 + GROUP - 1) / GROUP);
     const uint32_t gb = ib >= job.inputs ? 0 : min((nb + GROUP - 1) / GROUP, (job.inputs - ib + GROUP - 1) / GROUP);
+    uint32_t ga_far = 0, gb_far = 0;                                           // of a pair's second block (asked for by its first)
+    if (CG == 2) {
+        ga_far = o0 + 128 >= job.outputs ? 0 : min(2u, (job.outputs - o0 - 128 + GROUP - 1) / GROUP);
+        gb_far = ib + nb >= job.inputs ? 0 : min((nb + GROUP - 1) / GROUP, (job.inputs - ib - nb + GROUP - 1) / GROUP);
+    }
     const uint32_t smem = (smem_at(raw) + 1023u) & ~1023u;
-    const uint32_t a_bytes = 2 * GROUP_BYTES, stage_bytes = a_bytes + (nb + GROUP - 1) / GROUP * GROUP_BYTES;
+    const uint32_t pitch_group = job.ring * 128, shift_x = 2 * pitch_group;
     if (tid == 0) {
-        for (uint32_t s = 0; s < job.stages; s++) {
-            bar_init(&full[s], 2);
-            bar_init(&ready[s], CG);
+        for (uint32_t s = 0; s < SLOTS; s++) {
+            bar_init(&full[s], COPIES + 1 + CG);
+            bar_init(&part[s], COPIES);
             bar_init(&empty[s], 1);
         }
         for (int b = 0; b < 2; b++) {
@@ -281,7 +309,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
         bar_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 1) tmem_take<CG>(&tmem_base);
+    if (warp == PRODUCTS) tmem_take<CG>(&tmem_base);
     tmem_order_before();
     cluster.sync();
     tmem_order_after();
@@ -289,7 +317,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
 
     Cursor next{0, 0, 0, 0, 0};
     const int64_t r0 = (int64_t)job.rows * split / job.splits, r1 = (int64_t)job.rows * (split + 1) / job.splits;
-    if (warp == 3) {
+    if (warp == PLACES) {
         if (job.offsets) {
             // a sample goes to the split in whose share of the rows it begins
             next.k = split == 0 ? 0 : first_at(job.offsets, job.samples, r0);
@@ -300,118 +328,161 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
         }
     }
     bool well = true;
-    if (warp < 4) {
-        registers_less<72>();
-        uint32_t s = 0, turn = 0, uses[2] = {0, 0}, held = 1, b = 0;
+    if (warp < EPILOGUE) {
+        registers_less<48>();
+        uint32_t stage = 0;                  // of all so far
+        uint32_t at = 0;                     // its first row in the ring
+        uint32_t used = 0, held = 1, b = 0, parts = 0;
         for (;;) {
-            if (warp == 3) {
+            if (warp == PLACES) {
                 const uint32_t n = list_stages(list, next, job.offsets, (int32_t)job.rows, job.pairs);
                 if (lane == 0) listed = n;
             }
             block_meets();
             const uint32_t n = listed;
             if (n == 0) break;
-            if (warp == 0 || warp == 2) {
-                // copies of dy, and of x
-                const bool of_dy = warp == 0;
-                const uint32_t groups = of_dy ? ga : gb, shift = of_dy ? 0 : a_bytes;
+            Stage e = list[0];
+            if (warp < COPIES) {
+                // copies of every second group of dy, and of x
+                const bool of_dy = warp < 2;
+                const uint32_t odd = warp & 1u, groups = of_dy ? ga : gb, to = smem + (of_dy ? 0 : shift_x);
+                const uint32_t mine = (groups + 1 - odd) / 2, far = of_dy ? ga_far : gb_far, of_pair = mine + (far + 1 - odd) / 2;
                 const int32_t col = (int32_t)(of_dy ? o0 : ib);
-                const CUtensorMap *deep = of_dy ? &dy_deep : &x_deep, *brief = of_dy ? &dy_short : &x_short;
-                for (uint32_t i = 0; well && i < n; i++) {
-                    const Stage e = list[i];
-                    const uint32_t shorts = ((e.what & Stage::ROWS) + SHORT - 1) / SHORT, pair = e.what >> Stage::PAIR;
-                    const int32_t part = job.pairs == 1 ? 0 : (int32_t)(of_dy ? piece_of_dy(pair) : piece_of_x(pair));
-                    const uint32_t at = smem + s * stage_bytes + shift;
-                    if (!bar_wait(&empty[s], (turn & 1u) ^ 1u)) {
-                        well = false;
-                        break;
+                const CUtensorMap *map = of_dy ? maps.dy : maps.x;
+                uint32_t room = job.ring, oldest = 0;                          // the first stage of the list whose rows are not free yet
+                for (uint32_t i = 0; well && i < n; i++, stage++) {
+                    const uint32_t left = e.what & Stage::ROWS, pair = e.what >> Stage::PAIR, slot = stage % SLOTS, ends = left & 15u;
+                    const int32_t plane = job.pairs == 1 ? 0 : (int32_t)(of_dy ? piece_of_dy(pair) : piece_of_x(pair));
+                    const int32_t row = e.row;
+                    const uint32_t rows = (left + 15) & ~15u;
+                    e = list[i + 1];
+                    while (well && (room < rows || i - oldest >= SLOTS)) {
+                        const uint32_t was = stage - (i - oldest);
+                        well = bar_wait(&empty[was % SLOTS], was / SLOTS & 1u);
+                        room += ((list[oldest].what & Stage::ROWS) + 15) & ~15u;
+                        oldest++;
                     }
+                    if (!well) break;
+                    room -= rows;
                     if (elected()) {
-                        bar_expect(&full[s], groups * shorts * SHORT * 128);
-                        if (shorts == DEPTH / SHORT)
-                            for (uint32_t g = 0; g < groups; g++) tma_load(at + g * GROUP_BYTES, deep, col + (int32_t)(g * GROUP), e.row, part, &full[s]);
-                        else
-                            for (uint32_t h = 0; h < shorts; h++)
-                                for (uint32_t g = 0; g < groups; g++)
-                                    tma_load(at + g * GROUP_BYTES + h * SHORT * 128, brief, col + (int32_t)(g * GROUP), e.row + (int32_t)(h * SHORT), part, &full[s]);
+                        const uint32_t bar = ends ? smem_at(&part[slot]) : mapped(smem_at(&full[slot]), leader);
+                        if (ends) bar_expect(&part[slot], mine * rows * 128);
+                        else if (half == 0) bar_expect(&full[slot], of_pair * rows * 128);
+                        for (uint32_t done = 0, r = at; done < rows;) {
+                            const uint32_t fit = min(rows - done, job.ring - r), box = __clz((int)min(fit, DEPTH)) - 24, take = 128u >> box;   // fit: 16, 32, ...
+                            for (uint32_t g = odd; g < groups; g += 2)
+                                tma_load<CG>(to + g * pitch_group + r * 128, map + box, col + (int32_t)(g * GROUP), row + (int32_t)done, plane, bar);
+                            done += take;
+                            r = r + take == job.ring ? 0 : r + take;
+                        }
+                        if (ends && half == 0) bar_arrive(&full[slot], leader);
                     }
                     __syncwarp();
-                    if (++s == job.stages) s = 0, turn++;
+                    at += rows;
+                    if (at >= job.ring) at -= job.ring;
                 }
-            } else if (warp == 1) {
+                for (; well && oldest < n; oldest++) {
+                    const uint32_t was = stage - (n - oldest);
+                    well = bar_wait(&empty[was % SLOTS], was / SLOTS & 1u);
+                }
+            } else if (warp == PRODUCTS) {
                 if (half == 0)
-                    for (uint32_t i = 0; well && i < n; i++) {
-                        const Stage e = list[i];
-                        const uint32_t at = smem + s * stage_bytes, sixteens = ((e.what & Stage::ROWS) + 15) / 16;
-                        if (e.what & Stage::BEGINS) {
-                            if (e.what & Stage::FIRST) held ^= 1;
-                            b = e.what & Stage::FIRST ? held : held ^ 1;
-                            const uint32_t use = b ? uses[1]++ : uses[0]++;
-                            if (!bar_wait(&sum_empty[b], (use & 1u) ^ 1u)) well = false;
+                    for (uint32_t i = 0; well && i < n; i++, stage++) {
+                        const uint32_t what = e.what, slot = stage % SLOTS, sixteens = ((what & Stage::ROWS) + 15) / 16;
+                        e = list[i + 1];
+                        const bool begins = what & Stage::BEGINS;
+                        if (begins) {
+                            if (what & Stage::FIRST) held ^= 1;
+                            b = what & Stage::FIRST ? held : held ^ 1;
                         }
-                        if (!well || !bar_wait(&ready[s], turn & 1u)) {
+                        if (!bar_wait(&full[slot], stage / SLOTS & 1u)) {
                             well = false;
                             break;
                         }
                         tmem_order_after();
                         if (elected()) {
                             const uint32_t d = tmem + b * MOST_N;
-                            const uint64_t oa = operand(at), ob = operand(at + a_bytes);
-                            const bool add = !(e.what & Stage::BEGINS);
-                            if (sixteens == DEPTH / 16) {
+                            const uint64_t oa = operand(smem, job.ring), ob = operand(smem + shift_x, job.ring);
+                            if (sixteens == DEPTH / 16 && at + DEPTH <= job.ring) {
 #pragma unroll
-                                for (uint32_t h = 0; h < DEPTH / 16; h++) multiply<CG>(d, oa + h * (2048 >> 4), ob + h * (2048 >> 4), job.what, add || h);
+                                for (uint32_t h = 0; h < DEPTH / 16; h++)
+                                    multiply<CG>(d, oa + at * 8 + h * 128, ob + at * 8 + h * 128, job.what, !begins || h);
                             } else {
-                                for (uint32_t h = 0; h < sixteens; h++) multiply<CG>(d, oa + h * (2048 >> 4), ob + h * (2048 >> 4), job.what, add || h);
+                                uint32_t r = at;
+                                for (uint32_t h = 0; h < sixteens; h++) {
+                                    multiply<CG>(d, oa + r * 8, ob + r * 8, job.what, !begins || h);
+                                    r += 16;
+                                    if (r == job.ring) r = 0;
+                                }
                             }
-                            commit<CG>(&empty[s], (uint16_t)(3u << leader));
-                            if (e.what & Stage::ENDS) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
+                            commit<CG>(&empty[slot], (uint16_t)(3u << leader));
+                            if (what & Stage::ENDS) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
                         }
                         __syncwarp();
-                        if (++s == job.stages) s = 0, turn++;
+                        at += sixteens * 16;
+                        if (at >= job.ring) at -= job.ring;
                     }
+            } else if (warp == PLACES) {
+                // a place for a new sum; and for each block that nothing is to be cleared
+                for (uint32_t i = 0; well && i < n; i++, stage++) {
+                    const uint32_t what = e.what, slot = stage % SLOTS;
+                    e = list[i + 1];
+                    if (stage >= SLOTS) well = bar_wait(&empty[slot], stage / SLOTS & 1u ^ 1u);
+                    if (half == 0 && (what & Stage::BEGINS)) {
+                        if (what & Stage::FIRST) held ^= 1;
+                        b = what & Stage::FIRST ? held : held ^ 1;
+                        well = well && bar_wait(&sum_empty[b], (used >> b & 1u) ^ 1u);
+                        used ^= 1u << b;
+                    }
+                    if (well && elected()) {
+                        if (half == 0) bar_arrive(&full[slot], leader);
+                        if (!(what & 15u)) bar_arrive(&full[slot], leader);
+                    }
+                    __syncwarp();
+                }
             } else {
-                // Rows of the next sample, or none of any, that came with a sample's last ones count as zeros.
-                for (uint32_t i = 0; well && i < n; i++) {
-                    const uint32_t left = list[i].what & Stage::ROWS;
-                    if (!bar_wait(&full[s], turn & 1u)) {
-                        well = false;
-                        break;
-                    }
-                    if (left & 15u) {
-                        const uint32_t at = smem + s * stage_bytes + left * 128, words = (16 - (left & 15u)) * 8;
-                        for (uint32_t w = lane; w < words; w += 32) {
-                            for (uint32_t g = 0; g < ga; g++)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
-                            for (uint32_t g = 0; g < gb; g++)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + a_bytes + g * GROUP_BYTES + w * 16), "r"(0) : "memory");
+                // Rows of the next sample, or of none, that came with a sample's last ones count as zeros.  Two warps take these stages in turn; a lane
+                // has 16 bytes of the rows of a group.
+                for (uint32_t i = 0; well && i < n; i++, stage++) {
+                    const uint32_t left = e.what & Stage::ROWS, slot = stage % SLOTS, over = left & 15u;
+                    e = list[i + 1];
+                    if (over) {
+                        if ((held ^= 1) == warp - TAILS) {
+                            well = bar_wait(&part[slot], parts >> slot & 1u);
+                            if (!well) break;
+                            uint32_t from = at + left - over;    // the last sixteen rows: the ring's end is a multiple of 16
+                            if (from >= job.ring) from -= job.ring;
+                            for (uint32_t g = lane / 8; g < 2 + nb / GROUP; g += 4) {
+                                const uint32_t to = smem + g * pitch_group + from * 128 + lane % 8 * 16;
+#pragma unroll
+                                for (uint32_t r = 1; r < 16; r++)
+                                    if (r >= over) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(to + r * 128), "r"(0) : "memory");
+                            }
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                            if (elected()) bar_arrive(&full[slot], leader);
+                            __syncwarp();
                         }
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        parts ^= 1u << slot;
                     }
-                    __syncwarp();
-                    if (elected()) bar_arrive(&ready[s], leader);
-                    __syncwarp();
-                    if (++s == job.stages) s = 0, turn++;
+                    at += (left + 15) & ~15u;
+                    if (at >= job.ring) at -= job.ring;
                 }
             }
             block_meets();
         }
-        if (warp == 0 || warp == 2) {
-            // no copy is under way when the block ends: the last of each stage is waited for, whatever happened
-            for (uint32_t i = 0; i < job.stages; i++)
-                if (turn || i < s) {
-                    const uint32_t last = i < s ? turn : turn - 1;
-                    if (!bar_wait(&full[i], last & 1u)) well = false;
-                }
-        } else if (warp == 1) {
+        if (warp == PRODUCTS) {
             // products under way use both blocks' memory
             if (half == 0 && elected()) commit<CG>(&drained, (uint16_t)(3u << leader));
             __syncwarp();
             if (!bar_wait(&drained, 0)) well = false;
         }
+        // every copy that was waited for is there; after a wait that failed, copies under way get the time to end that they cannot need
+        if (!well)
+            for (int i = 0; i < 20; i++) __nanosleep(1000000);
         if (!well && lane == 0) atomicOr(job.status, STATUS_COPY);
         cluster.sync();                      // every product of the pair is done, and every sum read
-        if (warp == 1) {
+        if (warp == PRODUCTS) {
             tmem_order_after();
             tmem_give<CG>(tmem);
         }
@@ -420,27 +491,29 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
         return;
     }
     // the epilogue's warps: 32 lanes of tensor memory, half of a tile's columns
-    registers_more<216>();
+    registers_more<208>();
     float total[128];
 #pragma unroll
     for (int e = 0; e < 128; e++) total[e] = 0.0f;
-    const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - 4) / 4 * cols;
-    uint32_t uses[2] = {0, 0}, held = 1;
+    const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - EPILOGUE) / 4 * cols;
+    uint32_t used = 0, held = 1;
     for (;;) {
         block_meets();
         const uint32_t n = listed;
         if (n == 0) break;
+        uint32_t now = list[0].what;
         for (uint32_t i = 0; well && i < n; i++) {
-            const uint32_t what = list[i].what;
+            const uint32_t what = now;
+            now = list[i + 1].what;
             if (!(what & Stage::ENDS)) continue;
             const bool first = what & Stage::FIRST, last = what & Stage::LAST;
             if (first) held ^= 1;
             const uint32_t b = first ? held : held ^ 1;
-            const uint32_t use = b ? uses[1]++ : uses[0]++;
-            if (!bar_wait(&sum_full[b], use & 1u)) {
+            if (!bar_wait(&sum_full[b], used >> b & 1u)) {
                 well = false;
                 break;
             }
+            used ^= 1u << b;
             tmem_order_after();
             const uint32_t at = mine + b * MOST_N;
             if (first && last) {
@@ -489,7 +562,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     cluster.sync();                          // every product of the pair is done: the stages' memory takes the sums
     float *sums = reinterpret_cast<float *>(raw + (smem - smem_at(raw)));
     const uint32_t pitch = job.n + 1;
-    float *to = sums + ((warp & 3u) * 32 + lane) * pitch + (warp - 4) / 4 * cols;
+    float *to = sums + ((warp & 3u) * 32 + lane) * pitch + (warp - EPILOGUE) / 4 * cols;
 #pragma unroll
     for (int j = 0; j < 128; j += 32)
         if (j < cols)
@@ -499,7 +572,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     // the splits' sums, each block some outputs of its 128
     const uint32_t first = 128 * split / job.splits, behind = 128 * (split + 1) / job.splits;
     const uint32_t width = min(job.n, job.inputs - i0);
-    for (uint32_t o = first + warp - 4; o < behind; o += 8) {
+    for (uint32_t o = first + warp - EPILOGUE; o < behind; o += 8) {
         if (o0 + o >= job.outputs) break;
         float *out = job.weight + (size_t)(o0 + o) * job.inputs + i0;
         float v[MOST_N / 32];                // a row at once: loads from other blocks take long, stores should not wait for one another
@@ -618,9 +691,8 @@ Plan plan_of(const LinearMapArgs &a, uint32_t pairs, int n_sm) {
 }
 
 template <int CG>
-cudaError_t launch(const CUtensorMap (&m)[4], const LinearJob &job, uint32_t tiles, cudaStream_t s) {
-    const uint32_t stage = 2 * GROUP_BYTES + (job.n / CG + GROUP - 1) / GROUP * GROUP_BYTES;
-    const uint32_t bytes = (job.stages * stage > STAGING ? job.stages * stage : STAGING) + 1024;
+cudaError_t launch(const Maps &maps, const LinearJob &job, uint32_t tiles, cudaStream_t s) {
+    const uint32_t bytes = (RING_BYTES > STAGING ? RING_BYTES : STAGING) + 1024;
     cudaError_t rc = cudaFuncSetAttribute(linear_map_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (rc != cudaSuccess) return rc;
     cudaLaunchConfig_t cfg = {};
@@ -633,7 +705,7 @@ cudaError_t launch(const CUtensorMap (&m)[4], const LinearJob &job, uint32_t til
     at[0].val.clusterDim = {job.splits * CG, 1, 1};
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    rc = cudaLaunchKernelEx(&cfg, linear_map_kernel<CG>, m[0], m[1], m[2], m[3], job);
+    rc = cudaLaunchKernelEx(&cfg, linear_map_kernel<CG>, maps, job);
     return rc != cudaSuccess ? rc : FEDHE_LAUNCHED();
 }
 
@@ -677,12 +749,12 @@ cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *
     }
     const uint32_t pairs = parts == 3 ? 6 : 1;
     const Plan plan = plan_of(a, pairs, n_sm);
-    CUtensorMap m[4];
+    Maps maps;
     const bool half = dtype == HE_F16;
-    if (!tensor_map(m[0], dy.p, a.outputs, a.rows, dy.stride, parts, half, DEPTH) || !tensor_map(m[1], dy.p, a.outputs, a.rows, dy.stride, parts, half, SHORT) ||
-        !tensor_map(m[2], x.p, a.inputs, a.rows, x.stride, parts, half, DEPTH) || !tensor_map(m[3], x.p, a.inputs, a.rows, x.stride, parts, half, SHORT))
-        return cudaErrorInvalidValue;
-    const uint32_t stage = 2 * GROUP_BYTES + (plan.n / plan.cg + GROUP - 1) / GROUP * GROUP_BYTES;
+    for (int i = 0; i < BOXES; i++)
+        if (!tensor_map(maps.dy[i], dy.p, a.outputs, a.rows, dy.stride, parts, half, 128u >> i) ||
+            !tensor_map(maps.x[i], x.p, a.inputs, a.rows, x.stride, parts, half, 128u >> i))
+            return cudaErrorInvalidValue;
     LinearJob job{};
     job.offsets = alone ? nullptr : a.offsets;
     job.samples = a.samples;
@@ -692,8 +764,7 @@ cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *
     job.n = plan.n;
     job.splits = plan.splits;
     job.tiles_i = (uint32_t)((a.inputs + plan.n - 1) / plan.n);
-    job.stages = 196608 / stage;
-    if (job.stages > 8) job.stages = 8;
+    job.ring = RING_BYTES / (128 * (2 + plan.n / plan.cg / GROUP)) / 16 * 16;
     job.pairs = pairs;
     // fp32 sums; both operands fp16 or bf16, with the contracted index second; n columns, 128 rows for each block
     const uint32_t type = half ? 0 : 1;
@@ -702,7 +773,7 @@ cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *
     job.weight = a.weight;
     job.status = status;
     const uint32_t tiles = (uint32_t)((a.outputs + 128 * plan.cg - 1) / (128 * plan.cg)) * job.tiles_i;
-    return plan.cg == 1 ? launch<1>(m, job, tiles, s) : launch<2>(m, job, tiles, s);
+    return plan.cg == 1 ? launch<1>(maps, job, tiles, s) : launch<2>(maps, job, tiles, s);
 }
 
 }  // namespace fedhe
