@@ -34,7 +34,7 @@ constexpr uint32_t MOST_N = 256;                        // inputs of a tile; its
 constexpr uint32_t PIECE = 512, PIECE_ALONE = 128;
 // Warps by role: a stage's way through any of them takes some hundred clocks that nothing hides, so the work between copies and products
 // is spread over eight.
-constexpr uint32_t COPIES = 4, PRODUCTS = 4, PLACES = 5, TAILS = 6, EPILOGUE = 8;      // TAILS: two warps
+constexpr uint32_t COPIES = 4, PRODUCTS = 4, CHECKS = 5, EPILOGUE = 8;      // how many copy; the first warp of the others
 constexpr uint32_t THREADS = 512;
 constexpr uint32_t STAGING = 128 * (MOST_N + 1) * 4;
 constexpr uint32_t TRIES = 256;                         // of 10 ms at most
@@ -275,8 +275,7 @@ template <int CG>
 __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_constant__ Maps maps, const LinearJob job) {
     extern __shared__ uint8_t raw[];
     // A stage is full, in the block that issues the products, when that block's copying warps have arrived with what they and the other block's
-    // copy, when there is a place for its sum, and when each block has cleared what came with a sample's last rows; `part`: the block's copies
-    // of those.
+    // copy, and when each block has cleared what came with a sample's last rows; `part`: the block's copies of those.
     __shared__ uint64_t full[SLOTS], part[SLOTS], empty[SLOTS], sum_full[2], sum_empty[2], drained;
     __shared__ uint32_t tmem_base, listed;
     __shared__ alignas(8) Stage list[LISTED + 1];
@@ -298,7 +297,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
     const uint32_t pitch_group = job.ring * 128, shift_x = 2 * pitch_group;
     if (tid == 0) {
         for (uint32_t s = 0; s < SLOTS; s++) {
-            bar_init(&full[s], COPIES + 1 + CG);
+            bar_init(&full[s], COPIES + CG);
             bar_init(&part[s], COPIES);
             bar_init(&empty[s], 1);
         }
@@ -317,7 +316,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
 
     Cursor next{0, 0, 0, 0, 0};
     const int64_t r0 = (int64_t)job.rows * split / job.splits, r1 = (int64_t)job.rows * (split + 1) / job.splits;
-    if (warp == PLACES) {
+    if (warp == CHECKS) {
         if (job.offsets) {
             // a sample goes to the split in whose share of the rows it begins
             next.k = split == 0 ? 0 : first_at(job.offsets, job.samples, r0);
@@ -334,7 +333,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
         uint32_t at = 0;                     // its first row in the ring
         uint32_t used = 0, held = 1, b = 0, parts = 0;
         for (;;) {
-            if (warp == PLACES) {
+            if (warp == CHECKS) {
                 const uint32_t n = list_stages(list, next, job.offsets, (int32_t)job.rows, job.pairs);
                 if (lane == 0) listed = n;
             }
@@ -394,8 +393,10 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         if (begins) {
                             if (what & Stage::FIRST) held ^= 1;
                             b = what & Stage::FIRST ? held : held ^ 1;
+                            well = bar_wait(&sum_empty[b], (used >> b & 1u) ^ 1u);
+                            used ^= 1u << b;
                         }
-                        if (!bar_wait(&full[slot], stage / SLOTS & 1u)) {
+                        if (!well || !bar_wait(&full[slot], stage / SLOTS & 1u)) {
                             well = false;
                             break;
                         }
@@ -422,32 +423,14 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         at += sixteens * 16;
                         if (at >= job.ring) at -= job.ring;
                     }
-            } else if (warp == PLACES) {
-                // a place for a new sum; and for each block that nothing is to be cleared
-                for (uint32_t i = 0; well && i < n; i++, stage++) {
-                    const uint32_t what = e.what, slot = stage % SLOTS;
-                    e = list[i + 1];
-                    if (stage >= SLOTS) well = bar_wait(&empty[slot], stage / SLOTS & 1u ^ 1u);
-                    if (half == 0 && (what & Stage::BEGINS)) {
-                        if (what & Stage::FIRST) held ^= 1;
-                        b = what & Stage::FIRST ? held : held ^ 1;
-                        well = well && bar_wait(&sum_empty[b], (used >> b & 1u) ^ 1u);
-                        used ^= 1u << b;
-                    }
-                    if (well && elected()) {
-                        if (half == 0) bar_arrive(&full[slot], leader);
-                        if (!(what & 15u)) bar_arrive(&full[slot], leader);
-                    }
-                    __syncwarp();
-                }
             } else {
-                // Rows of the next sample, or of none, that came with a sample's last ones count as zeros.  Two warps take these stages in turn; a lane
+                // Rows of the next sample, or of none, that came with a sample's last ones count as zeros.  Three warps take the stages in turn; a lane
                 // has 16 bytes of the rows of a group.
                 for (uint32_t i = 0; well && i < n; i++, stage++) {
                     const uint32_t left = e.what & Stage::ROWS, slot = stage % SLOTS, over = left & 15u;
                     e = list[i + 1];
-                    if (over) {
-                        if ((held ^= 1) == warp - TAILS) {
+                    if (stage % (EPILOGUE - CHECKS) == warp - CHECKS) {
+                        if (over) {
                             well = bar_wait(&part[slot], parts >> slot & 1u);
                             if (!well) break;
                             uint32_t from = at + left - over;    // the last sixteen rows: the ring's end is a multiple of 16
@@ -460,11 +443,14 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                             }
                             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                             __syncwarp();
-                            if (elected()) bar_arrive(&full[slot], leader);
-                            __syncwarp();
+                        } else if (stage >= SLOTS) {
+                            // the slot's last stage is done with
+                            well = bar_wait(&empty[slot], stage / SLOTS & 1u ^ 1u);
                         }
-                        parts ^= 1u << slot;
+                        if (well && elected()) bar_arrive(&full[slot], leader);
+                        __syncwarp();
                     }
+                    if (over) parts ^= 1u << slot;
                     at += (left + 15) & ~15u;
                     if (at >= job.ring) at -= job.ring;
                 }
@@ -496,6 +482,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
 #pragma unroll
     for (int e = 0; e < 128; e++) total[e] = 0.0f;
     const uint32_t cols = job.n / 2, mine = tmem + ((warp & 3u) << 21) + (warp - EPILOGUE) / 4 * cols;
+    const auto free_place = [&](uint32_t b) {
+        tmem_order_before();
+        __syncwarp();
+        if (elected()) bar_arrive(&sum_empty[b], leader);
+        __syncwarp();
+    };
     uint32_t used = 0, held = 1;
     for (;;) {
         block_meets();
@@ -522,11 +514,13 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                     if (j + 64 <= cols) {
                         float v[64];
                         tmem_get64(at + j, v);
+                        if (j + 64 == cols) free_place(b);       // before what was read last is added
 #pragma unroll
                         for (int e = 0; e < 64; e++) total[j + e] += fabsf(v[e]);
                     } else if (j < cols) {
                         float v[32];
                         tmem_get32(at + j, v);
+                        free_place(b);
 #pragma unroll
                         for (int e = 0; e < 32; e++) total[j + e] += fabsf(v[e]);
                     }
@@ -548,12 +542,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                             tmem_put16(mine + held * MOST_N + j, u);
                         }
                     }
-            }
-            tmem_order_before();
-            __syncwarp();
-            if (elected()) {
-                if (!first || last) bar_arrive(&sum_empty[b], leader);
-                if (!first && last) bar_arrive(&sum_empty[held], leader);
+                free_place(b);
+                if (last) free_place(held);
             }
         }
         block_meets();
