@@ -51,7 +51,8 @@ struct NormArgs {
     MatOut y;
     float *mean, *rstd;
 };
-cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, cudaStream_t s);
+// status (of these and of launch_linear_map): the context's, raised where something inside a kernel does not arrive
+cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 // How rows are summed: all of them, or within a sample with the magnitudes added over the samples, or every row a sample of its own.
 enum class SumOver { ALL, SAMPLES, ROWS };
@@ -70,7 +71,7 @@ struct NormGradArgs {
     void *work;
 };
 size_t norm_grad_work_bytes(size_t rows, size_t width, int n_sm);
-cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, cudaStream_t s);
+cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 // Sums of the columns of a matrix, dst (+)= the sums; work of column_sums_work_bytes()
 struct ColumnSumArgs {
@@ -99,7 +100,6 @@ struct LinearMapArgs {
 // whether the kernels can read a matrix where it lies
 bool linear_map_aligned(const MatArg &m, size_t width, int dtype);
 size_t linear_map_work_bytes(size_t rows, size_t inputs, size_t outputs, int dtype, bool samples, bool aligned, bool bias, int n_sm);
-// status: the context's, raised where something inside the kernel does not arrive
 cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 }  // namespace fedhe

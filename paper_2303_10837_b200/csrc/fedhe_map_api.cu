@@ -75,7 +75,7 @@ int he_layer_norm(he_ctx *ctx, const void *x_dev, int dtype, size_t rows, size_t
         return HE_ERR_INVALID_ARG;
     if (x_dev == y_dev && rows > 1 && x_stride != y_stride) return HE_ERR_INVALID_ARG;
     const NormArgs a{{x_dev, x_stride}, rows, width, weight_dev, bias_dev, weight_dtype, eps, {y_dev, y_stride}, mean_dev, rstd_dev};
-    return done(launch_norm(a, dtype, ctx->sm_count, as_stream(stream)));
+    return done(launch_norm(a, dtype, ctx->sm_count, ctx->dev.status, as_stream(stream)));
 }
 
 size_t he_layer_norm_backward_work_bytes(const he_ctx *ctx, size_t rows, size_t width) {
@@ -98,7 +98,7 @@ int he_layer_norm_backward(he_ctx *ctx, const void *dy_dev, size_t dy_stride, co
     if (rows && (dx_dev == x_dev || dx_dev == dy_dev)) return HE_ERR_INVALID_ARG;
     const NormGradArgs a{{dy_dev, dy_stride}, {x_dev, x_stride}, rows, width, mean_dev, rstd_dev, weight_dev, weight_dtype,
                          samples_dev ? SumOver::SAMPLES : SumOver::ALL, samples_dev, (uint32_t)num_samples, {dx_dev, dx_stride}, dweight_dev, dbias_dev, work_dev};
-    return done(launch_norm_grad(a, dtype, ctx->sm_count, as_stream(stream)));
+    return done(launch_norm_grad(a, dtype, ctx->sm_count, ctx->dev.status, as_stream(stream)));
 }
 
 size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs, int samples, int aligned) {

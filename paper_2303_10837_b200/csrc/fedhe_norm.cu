@@ -138,50 +138,108 @@ struct RunsOut {
 
 // ---- a row at a time, held in registers ----
 
-// How a row is shared out: `threads` threads (a multiple of 32), each with K packs, `groups` of them in a block.
-constexpr int HELD = 16;                                     // elements of a thread
-constexpr uint32_t FORWARD_THREADS = 256, BACK_THREADS = 512;
+// How a row is shared out: `threads` threads (a multiple of 32), each with `held` elements, `groups` of them in a block.  A group's rows come to
+// shared memory by bulk copies, `depth` rows ahead: that many loads in registers would leave room for few warps (rows one ahead in
+// registers: 176 us for 32768 rows of 4096 in bf16, by copies ...).
 struct RowPlan {
-    uint32_t threads, groups;
+    uint32_t threads, groups, depth;
+    uint32_t room;                                           // bytes of a row in shared memory
 };
+constexpr uint32_t MOST_DEPTH = 8;
 // false: the row is too long for one block
-inline bool plan_row(size_t width, uint32_t block, RowPlan &p) {
-    const size_t t = (width + HELD - 1) / HELD;
+inline bool plan_row(size_t width, size_t element, uint32_t block, uint32_t held, uint32_t rows_at_once, size_t ring, RowPlan &p) {
+    const size_t t = (width + held - 1) / held;
     if (t > block) return false;
     p.threads = (uint32_t)(t + 31) / 32 * 32;
     p.groups = block / p.threads;
-    return true;
+    p.room = (uint32_t)((width * element + 15) / 16 * 16 + 16);
+    const size_t depth = ring / ((size_t)p.groups * rows_at_once * p.room);
+    p.depth = (uint32_t)(depth < MOST_DEPTH ? depth : MOST_DEPTH);
+    return p.depth > 0;
 }
 
 __device__ __forceinline__ void group_sync(uint32_t group, uint32_t threads) {
-    asm volatile("barrier.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
-}
-// Sums over a group's threads, of N values each; `at`: a place of 32 N words that the group's last call but one used.
-template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float *at, uint32_t group, uint32_t threads) {
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = warp_sum(v[i]);
-    if (threads == 32) return;
-    const uint32_t t = threadIdx.x - group * threads, warps = threads / 32, lane = t & 31u;
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < N; i++) at[i * 32 + t / 32] = v[i];
-    group_sync(group, threads);
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = warp_sum(lane < warps ? at[i * 32 + lane] : 0.0f);
+    if (threads == 32) __syncwarp();
+    else asm volatile("barrier.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
 }
 
-template <class T, int V, int K>
-__device__ __forceinline__ void load_row(Pack<T, V> (&p)[K], const T *row, uint32_t t, uint32_t threads, uint32_t width) {
-#pragma unroll
-    for (int k = 0; k < K; k++) {
-        const uint32_t c = (k * threads + t) * V;
-        if (c < width) p[k] = load_pack<T, V>(row + c);
-        else
-#pragma unroll
-            for (int e = 0; e < V; e++) p[k].v[e] = from_f32<T>(0.0f);
+// The rows of a matrix as copies see them: whole 16 bytes, none outside the memory that the matrix spans.
+template <class T>
+struct Rows {
+    const T *p;
+    size_t stride;
+    uintptr_t low, high;                                     // whole 16 bytes of the matrix
+    uint32_t bytes;                                          // of a row
+    __device__ __forceinline__ Rows(const MatArg &m, size_t rows, uint32_t width) : p(static_cast<const T *>(m.p)), stride(m.stride), bytes(width * (uint32_t)sizeof(T)) {
+        low = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15;
+        high = (reinterpret_cast<uintptr_t>(p + (rows - 1) * stride) + bytes) & ~(uintptr_t)15;
     }
+    __device__ __forceinline__ uintptr_t at(size_t r) const { return reinterpret_cast<uintptr_t>(p + r * stride); }
+    // what is copied of a row
+    __device__ __forceinline__ uintptr_t from(size_t r) const {
+        const uintptr_t a = at(r) & ~(uintptr_t)15;
+        return a < low ? low : a;
+    }
+    __device__ __forceinline__ uint32_t size(size_t r) const {
+        uintptr_t e = (at(r) + bytes + 15) & ~(uintptr_t)15;
+        if (e > high) e = high;
+        return e > from(r) ? (uint32_t)(e - from(r)) : 0;
+    }
+    __device__ __forceinline__ void copy(size_t r, uint8_t *room, uint64_t *bar) const {
+        const uint32_t n = size(r);
+        if (!n) return;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(room) + (uint32_t)(from(r) - (at(r) & ~(uintptr_t)15));
+        asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from(r)), "r"(n),
+                     "r"((uint32_t)__cvta_generic_to_shared(bar))
+                     : "memory");
+    }
+    // A thread's packs of a row that has been copied; zeros behind its end.  A matrix's first and last bytes that no copy brings come from where they are.
+    template <int V, int K>
+    __device__ __forceinline__ void get(Pack<T, V> (&v)[K], size_t r, const uint8_t *room, uint32_t t, uint32_t threads, uint32_t width) const {
+        const T *row = reinterpret_cast<const T *>(room + (at(r) & 15));
+        const bool whole = from(r) <= at(r) && from(r) + size(r) >= at(r) + bytes;
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            const uint32_t c = (k * threads + t) * V;
+            if (c < width) v[k] = load_pack<T, V>(row + c);
+            else
+#pragma unroll
+                for (int e = 0; e < V; e++) v[k].v[e] = from_f32<T>(0.0f);
+        }
+        if (!whole)
+#pragma unroll
+            for (int k = 0; k < K; k++)
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const uint32_t c = (k * threads + t) * V + e;
+                    const uintptr_t x = at(r) + c * sizeof(T);
+                    if (c < width && (x < from(r) || x >= from(r) + size(r))) v[k].v[e] = p[r * stride + c];
+                }
+    }
+};
+
+__device__ __forceinline__ void copies_begin(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(bar)), "r"(bytes) : "memory");
 }
+constexpr uint32_t COPY_TRIES = 256;             // of 10 ms at most
+__device__ __forceinline__ bool copies_done(uint64_t *bar, uint32_t parity) {
+    for (uint32_t i = 0; i < COPY_TRIES; i++) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"((uint32_t)__cvta_generic_to_shared(bar)), "r"(parity)
+                     : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+
+// Copies that did not come in time have 20 ms more before their memory is given up.
+__device__ __noinline__ void copies_lost(int *status) {
+    atomicOr(status, STATUS_COPY);
+    for (int i = 0; i < 20; i++) __nanosleep(1000000);
+}
+
 template <int V, int K>
 __device__ __forceinline__ void load_weights(float (&w)[K][V], const void *p, int type, float otherwise, uint32_t t, uint32_t threads, uint32_t width) {
 #pragma unroll
@@ -193,44 +251,85 @@ __device__ __forceinline__ void load_weights(float (&w)[K][V], const void *p, in
         }
 }
 
-// Groups of threads take rows in turn; the weights stay in registers, and a row is asked for while the one before it is worked on.  Bounded by
-// memory: 32768 rows of 4096 in bf16 ...
-template <class T, int V>
-__global__ void __launch_bounds__(FORWARD_THREADS, 3) norm_kernel(const NormArgs a, const RowPlan plan) {
+// Mean and sum of squared differences from it of `n` values; two of them join to that of all (Chan, Golub and LeVeque's formula), so that
+// threads need to meet once for a row, and nothing is lost where the mean is large.
+struct Spread {
+    float n, mean, m2;
+    __device__ __forceinline__ void join(float on, float om, float o2) {
+        const float all = n + on, share = n > 0.0f ? __fdividef(on, all) : 1.0f, d = om - mean;
+        m2 += o2 + d * d * n * share;
+        mean = n > 0.0f ? fmaf(d, share, mean) : om;
+        n = all;
+    }
+};
+
+// Groups of threads take rows in turn; the weights stay in registers.
+template <class T, int V, int HELD, int THREADS, int BLOCKS>
+__global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a, const RowPlan plan, int *status) {
     constexpr int K = HELD / V;
-    __shared__ float sums[2][8][32];
-    const uint32_t group = threadIdx.x / plan.threads, t = threadIdx.x % plan.threads, width = (uint32_t)a.width;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ uint64_t bars[THREADS / 32][MOST_DEPTH];
+    __shared__ Spread met[2][THREADS / 32];
+    const uint32_t group = threadIdx.x / plan.threads, t = threadIdx.x % plan.threads, width = (uint32_t)a.width, lane = t & 31u;
     if (group >= plan.groups) return;
-    const size_t step = (size_t)gridDim.x * plan.groups;
-    size_t r = (size_t)blockIdx.x * plan.groups + group;
-    Pack<T, V> next[K];
-    if (r < a.rows) load_row<T, V, K>(next, static_cast<const T *>(a.x.p) + r * a.x.stride, t, plan.threads, width);
+    const size_t step = (size_t)gridDim.x * plan.groups, first = (size_t)blockIdx.x * plan.groups + group;
+    const Rows<T> rows(a.x, a.rows, width);
+    uint8_t *mine = ring + (size_t)group * plan.depth * plan.room;
+    if (t == 0) {
+        for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bars[group][d])) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (uint32_t d = 0; d < plan.depth && first + d * step < a.rows; d++) {
+            copies_begin(&bars[group][d], rows.size(first + d * step));
+            rows.copy(first + d * step, mine + d * plan.room, &bars[group][d]);
+        }
+    }
     float w[K][V], b[K][V];
     load_weights<V, K>(w, a.weight, a.weight_type, 1.0f, t, plan.threads, width);
     load_weights<V, K>(b, a.bias, a.weight_type, 0.0f, t, plan.threads, width);
-    const float n = (float)a.width;
-    for (; r < a.rows; r += step) {
-        float x[K][V], s[1] = {0.0f};
+    uint32_t held = 0;                                       // elements of this thread
+#pragma unroll
+    for (int k = 0; k < K; k++) held += (k * plan.threads + t) * V < width ? V : 0;
+    const uint32_t warps = plan.threads / 32, w0 = group * warps;
+    group_sync(group, plan.threads);
+    uint32_t d = 0, turn = 0, odd = 0;
+    bool lost = false;                                       // a copy did not come: none is waited for any more
+    for (size_t r = first; r < a.rows; r += step) {
+        if (!lost && !copies_done(&bars[group][d], turn)) lost = true;
+        Pack<T, V> p[K];
+        rows.get(p, r, mine + d * plan.room, t, plan.threads, width);
+        float x[K][V], sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < K; k++)
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                x[k][e] = to_f32(next[k].v[e]);
-                s[0] += x[k][e];
+                x[k][e] = to_f32(p[k].v[e]);
+                sum += x[k][e];
             }
-        if (r + step < a.rows) load_row<T, V, K>(next, static_cast<const T *>(a.x.p) + (r + step) * a.x.stride, t, plan.threads, width);
-        group_sum<1>(s, sums[0][group], group, plan.threads);
-        const float mean = s[0] / n;
-        s[0] = 0.0f;
+        Spread s{(float)held, held ? sum / (float)held : 0.0f, 0.0f};
 #pragma unroll
         for (int k = 0; k < K; k++)
 #pragma unroll
-            for (int e = 0; e < V; e++) {
-                x[k][e] -= mean;
-                if ((k * plan.threads + t) * V + (V == 1 ? 0 : e) < width) s[0] = fmaf(x[k][e], x[k][e], s[0]);
-            }
-        group_sum<1>(s, sums[1][group], group, plan.threads);
-        const float rstd = 1.0f / sqrtf(s[0] / n + a.eps);
+            for (int e = 0; e < V; e++)
+                if ((k * plan.threads + t) * V < width) {
+                    const float q = x[k][e] - s.mean;
+                    s.m2 = fmaf(q, q, s.m2);
+                }
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+            s.join(__shfl_xor_sync(0xffffffffu, s.n, o), __shfl_xor_sync(0xffffffffu, s.mean, o), __shfl_xor_sync(0xffffffffu, s.m2, o));
+        if (lane == 0) met[odd][threadIdx.x / 32] = s;
+        group_sync(group, plan.threads);                     // and the row is in registers: its place takes another
+        if (t == 0 && r + plan.depth * step < a.rows) {
+            copies_begin(&bars[group][d], rows.size(r + plan.depth * step));
+            rows.copy(r + plan.depth * step, mine + d * plan.room, &bars[group][d]);
+        }
+        s = lane < warps ? met[odd][w0 + lane] : Spread{0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+            s.join(__shfl_xor_sync(0xffffffffu, s.n, o), __shfl_xor_sync(0xffffffffu, s.mean, o), __shfl_xor_sync(0xffffffffu, s.m2, o));
+        // the lanes joined in different orders: the first one's result is everyone's
+        s.mean = __shfl_sync(0xffffffffu, s.mean, 0);
+        const float rstd = 1.0f / sqrtf(__shfl_sync(0xffffffffu, s.m2, 0) / (float)width + a.eps);
         T *y = static_cast<T *>(a.y.p) + r * a.y.stride;
 #pragma unroll
         for (int k = 0; k < K; k++) {
@@ -238,46 +337,58 @@ __global__ void __launch_bounds__(FORWARD_THREADS, 3) norm_kernel(const NormArgs
             if (c >= width) continue;
             Pack<T, V> o;
 #pragma unroll
-            for (int e = 0; e < V; e++) o.v[e] = from_f32<T>(fmaf(x[k][e] * rstd, w[k][e], b[k][e]));
+            for (int e = 0; e < V; e++) o.v[e] = from_f32<T>(fmaf((x[k][e] - s.mean) * rstd, w[k][e], b[k][e]));
             store_pack<T, V>(y + c, o);
         }
         if (t == 0) {
-            a.mean[r] = mean;
+            a.mean[r] = s.mean;
             a.rstd[r] = rstd;
         }
+        odd ^= 1u;
+        if (++d == plan.depth) d = 0, turn ^= 1u;
     }
+    if (lost) copies_lost(status);
 }
 
 // The backward pass.  A block takes a run of rows, its groups parts of it in order; sums over rows stay in registers, and go to shared
 // memory where a sample ends.  What the block leaves is a run's head, inner part and tail of every column (see Run).
-template <class T, int V, bool SAMPLES>
-__global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGradArgs a, const RowPlan plan, const RunsOut out) {
+constexpr uint32_t BACK_THREADS = 512;
+template <class T, int V, int HELD, bool SAMPLES>
+__global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGradArgs a, const RowPlan plan, const RunsOut out, int *status) {
     constexpr int K = HELD / V;
-    extern __shared__ float parts[];                 // [head, inner, tail][groups][2 planes][width]; without samples heads only
-    __shared__ float sums[2][16][64];
-    __shared__ int cuts[16];
-    const uint32_t group = threadIdx.x / plan.threads, t = threadIdx.x % plan.threads, width = (uint32_t)a.width, run = blockIdx.x;
+    // heads and inner parts, [groups][2 planes][width] each; then the ring, where the tails go when it is done with.  Without samples the ring, then heads.
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ uint64_t bars[BACK_THREADS / 32][MOST_DEPTH];
+    __shared__ float2 met[2][BACK_THREADS / 32];
+    __shared__ int cuts[BACK_THREADS / 32];
+    const uint32_t group = threadIdx.x / plan.threads, t = threadIdx.x % plan.threads, width = (uint32_t)a.width, run = blockIdx.x, lane = t & 31u;
     const size_t lo = a.rows * run / out.runs, hi = a.rows * (run + 1) / out.runs;
-    const auto part = [&](int what, uint32_t g, int plane) { return parts + ((size_t)(what * plan.groups + g) * 2 + plane) * width; };
+    const size_t plane_words = (size_t)plan.groups * 2 * width;
+    float *heads = reinterpret_cast<float *>(ring), *inners = heads + plane_words, *tails = SAMPLES ? inners + plane_words : heads;
+    uint8_t *copies = SAMPLES ? ring + (2 * plane_words * sizeof(float) + 15) / 16 * 16 : ring;
+    const auto place = [&](float *of, uint32_t g, int plane) { return of + ((size_t)g * 2 + plane) * width; };
+    int cut = 0;
+    float sw[K][V], sb[K][V];
+#pragma unroll
+    for (int k = 0; k < K; k++)
+#pragma unroll
+        for (int e = 0; e < V; e++) sw[k][e] = sb[k][e] = 0.0f;
     if (group < plan.groups) {
         const size_t begin = lo + (hi - lo) * group / plan.groups, end = lo + (hi - lo) * (group + 1) / plan.groups;
-        const T *xs = static_cast<const T *>(a.x.p), *dys = static_cast<const T *>(a.dy.p);
-        Pack<T, V> xn[K], gn[K];
-        float mean_n = 0.0f, rstd_n = 0.0f;
-        if (begin < end) {
-            load_row<T, V, K>(xn, xs + begin * a.x.stride, t, plan.threads, width);
-            load_row<T, V, K>(gn, dys + begin * a.dy.stride, t, plan.threads, width);
-            mean_n = a.mean[begin];
-            rstd_n = a.rstd[begin];
+        const Rows<T> xs(a.x, a.rows, width), dys(a.dy, a.rows, width);
+        uint8_t *mine = copies + (size_t)group * plan.depth * 2 * plan.room;
+        const auto fetch = [&](size_t r, uint32_t d) {
+            copies_begin(&bars[group][d], xs.size(r) + dys.size(r));
+            xs.copy(r, mine + d * 2 * plan.room, &bars[group][d]);
+            dys.copy(r, mine + (d * 2 + 1) * plan.room, &bars[group][d]);
+        };
+        if (t == 0) {
+            for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bars[group][d])) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            for (uint32_t d = 0; d < plan.depth && begin + d < end; d++) fetch(begin + d, d);
         }
-        float w[K][V], sw[K][V], sb[K][V];
+        float w[K][V];
         load_weights<V, K>(w, a.weight, a.weight_type, 1.0f, t, plan.threads, width);
-#pragma unroll
-        for (int k = 0; k < K; k++)
-#pragma unroll
-            for (int e = 0; e < V; e++) sw[k][e] = sb[k][e] = 0.0f;
-        const float n = 1.0f / (float)a.width;
-        int cut = 0;
         SampleWalk walk;
         walk.begin = 0;
         walk.end = INT64_MAX;
@@ -290,12 +401,12 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
                     const uint32_t c = (k * plan.threads + t) * V + e;
                     if (c < width) {
                         if (cut) {
-                            part(1, group, 0)[c] += fabsf(sw[k][e]);
-                            part(1, group, 1)[c] += fabsf(sb[k][e]);
+                            place(inners, group, 0)[c] += fabsf(sw[k][e]);
+                            place(inners, group, 1)[c] += fabsf(sb[k][e]);
                         } else {
-                            part(0, group, 0)[c] = sw[k][e];
-                            part(0, group, 1)[c] = sb[k][e];
-                            part(1, group, 0)[c] = part(1, group, 1)[c] = 0.0f;
+                            place(heads, group, 0)[c] = sw[k][e];
+                            place(heads, group, 1)[c] = sb[k][e];
+                            place(inners, group, 0)[c] = place(inners, group, 1)[c] = 0.0f;
                         }
                     }
                     sw[k][e] = sb[k][e] = 0.0f;
@@ -306,25 +417,38 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
             walk.seek(a.offsets, a.samples, (int64_t)begin);
             if (walk.begin == (int64_t)begin) close();       // the run before this one ends with another sample
         }
+        const uint32_t warps = plan.threads / 32, w0 = group * warps;
+        const float n = 1.0f / (float)width;
+        float mean_next = begin < end ? a.mean[begin] : 0.0f, rstd_next = begin < end ? a.rstd[begin] : 0.0f;
+        group_sync(group, plan.threads);
+        uint32_t d = 0, turn = 0;
+        bool lost = false;
         for (size_t r = begin; r < end; r++) {
-            float x[K][V], g[K][V], s[2] = {0.0f, 0.0f};
-            const float mean = mean_n, rstd = rstd_n;
-#pragma unroll
-            for (int k = 0; k < K; k++)
-#pragma unroll
-                for (int e = 0; e < V; e++) {
-                    x[k][e] = (to_f32(xn[k].v[e]) - mean) * rstd;
-                    g[k][e] = to_f32(gn[k].v[e]);
-                    const float q = g[k][e] * w[k][e];       // behind the row's end g is 0
-                    s[0] += q;
-                    s[1] = fmaf(q, x[k][e], s[1]);
-                }
+            const float mean = mean_next, rstd = rstd_next;
             if (r + 1 < end) {
-                load_row<T, V, K>(xn, xs + (r + 1) * a.x.stride, t, plan.threads, width);
-                load_row<T, V, K>(gn, dys + (r + 1) * a.dy.stride, t, plan.threads, width);
-                mean_n = a.mean[r + 1];
-                rstd_n = a.rstd[r + 1];
+                mean_next = a.mean[r + 1];
+                rstd_next = a.rstd[r + 1];
             }
+            if (!lost && !copies_done(&bars[group][d], turn)) lost = true;
+            float x[K][V], g[K][V], s0 = 0.0f, s1 = 0.0f;
+            {
+                Pack<T, V> px[K], pg[K];
+                xs.get(px, r, mine + d * 2 * plan.room, t, plan.threads, width);
+                dys.get(pg, r, mine + (d * 2 + 1) * plan.room, t, plan.threads, width);
+#pragma unroll
+                for (int k = 0; k < K; k++)
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        x[k][e] = (to_f32(px[k].v[e]) - mean) * rstd;
+                        g[k][e] = to_f32(pg[k].v[e]);
+                        const float q = g[k][e] * w[k][e];   // behind the row's end g is 0
+                        s0 += q;
+                        s1 = fmaf(q, x[k][e], s1);
+                    }
+            }
+            s0 = warp_sum(s0);
+            s1 = warp_sum(s1);
+            if (lane == 0) met[r & 1][threadIdx.x / 32] = make_float2(s0, s1);
             if (SAMPLES && (int64_t)r >= walk.end) {
                 close();
                 walk.next((int64_t)r);
@@ -338,8 +462,10 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
                         sb[k][e] += g[k][e];
                     }
             }
-            group_sum<2>(s, sums[r & 1][group], group, plan.threads);
-            const float ma = s[0] * n, man = s[1] * n;
+            group_sync(group, plan.threads);                 // and the rows are in registers: their places take others
+            if (t == 0 && r + plan.depth < end) fetch(r + plan.depth, d);
+            const float2 of = lane < warps ? met[r & 1][w0 + lane] : make_float2(0.0f, 0.0f);
+            const float ma = warp_sum(of.x) * n, man = warp_sum(of.y) * n;
             T *dx = static_cast<T *>(a.dx.p) + r * a.dx.stride;
 #pragma unroll
             for (int k = 0; k < K; k++) {
@@ -350,16 +476,22 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
                 for (int e = 0; e < V; e++) o.v[e] = from_f32<T>(rstd * (fmaf(g[k][e], w[k][e], -ma) - x[k][e] * man));
                 store_pack<T, V>(dx + c, o);
             }
+            if (++d == plan.depth) d = 0, turn ^= 1u;
         }
+        if (lost) copies_lost(status);
+    }
+    __syncthreads();                                         // the ring is done with
+    if (group < plan.groups) {
         // what is left is the tail, or the head of a run without a cut
+        float *to = SAMPLES && cut ? tails : heads;
 #pragma unroll
         for (int k = 0; k < K; k++)
 #pragma unroll
             for (int e = 0; e < V; e++) {
                 const uint32_t c = (k * plan.threads + t) * V + e;
                 if (c < width) {
-                    part(cut ? 2 : 0, group, 0)[c] = sw[k][e];
-                    part(cut ? 2 : 0, group, 1)[c] = sb[k][e];
+                    place(to, group, 0)[c] = sw[k][e];
+                    place(to, group, 1)[c] = sb[k][e];
                 }
             }
         if (SAMPLES && t == 0) cuts[group] = cut;
@@ -370,9 +502,9 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
         const uint32_t c = plane ? i - width : i;
         Run all{0.0f, 0.0f, 0.0f, 0};
         for (uint32_t g = 0; g < plan.groups; g++) {
-            if (!SAMPLES) all.head += part(0, g, plane)[c];
-            else if (cuts[g]) all.join(Run{part(0, g, plane)[c], part(1, g, plane)[c], part(2, g, plane)[c], 1});
-            else all.join(Run{part(0, g, plane)[c], 0.0f, 0.0f, 0});
+            if (!SAMPLES) all.head += place(heads, g, plane)[c];
+            else if (cuts[g]) all.join(Run{place(heads, g, plane)[c], place(inners, g, plane)[c], place(tails, g, plane)[c], 1});
+            else all.join(Run{place(heads, g, plane)[c], 0.0f, 0.0f, 0});
         }
         out.of(run, 0, plane)[c] = all.head;
         if (SAMPLES) {
@@ -550,48 +682,68 @@ cudaError_t sums(const MatArg &m, const MatArg &x, const float *mean, const floa
 
 inline uint32_t row_threads(size_t packs) { return packs >= 256 ? 256 : (uint32_t)(packs + 31) / 32 * 32; }
 
+// Shared memory of a block: all that there is less what the kernels hold besides, for as many blocks as share an SM.
+constexpr size_t SHARED = 220 << 10;
+
+template <class T, int V, int HELD, int THREADS, int BLOCKS>
+bool norm_go(const NormArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
+    RowPlan plan;
+    if (!plan_row(a.width, sizeof(T), THREADS, HELD, 1, SHARED / BLOCKS - 4096, plan)) return false;
+    const auto kernel = norm_kernel<T, V, HELD, THREADS, BLOCKS>;
+    const size_t bytes = (size_t)plan.groups * plan.depth * plan.room, blocks = (a.rows + plan.groups - 1) / plan.groups, most = (size_t)BLOCKS * n_sm;
+    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (rc != cudaSuccess) return true;
+    kernel<<<(unsigned)(blocks < most ? blocks : most), THREADS, bytes, s>>>(a, plan, status);
+    rc = FEDHE_LAUNCHED();
+    return true;
+}
+
 template <class T>
-cudaError_t norm_of(const NormArgs &a, int n_sm, cudaStream_t s) {
+cudaError_t norm_of(const NormArgs &a, int n_sm, int *status, cudaStream_t s) {
     if (a.rows == 0) return cudaSuccess;
     const bool wide = wide_rows<T>(a.x.p, a.x.stride, a.width) && wide_rows<T>(a.y.p, a.y.stride, a.width);
-    RowPlan plan;
-    if (plan_row(a.width, FORWARD_THREADS, plan)) {
-        const size_t blocks = (a.rows + plan.groups - 1) / plan.groups, most = (size_t)3 * n_sm;
-        const unsigned grid = (unsigned)(blocks < most ? blocks : most);
-        if (wide) norm_kernel<T, WIDE<T>><<<grid, FORWARD_THREADS, 0, s>>>(a, plan);
-        else norm_kernel<T, 1><<<grid, FORWARD_THREADS, 0, s>>>(a, plan);
-    } else if (wide) {
-        norm_long_kernel<T, WIDE<T>><<<(unsigned)a.rows, row_threads(a.width / WIDE<T>), 0, s>>>(a);
-    } else {
-        norm_long_kernel<T, 1><<<(unsigned)a.rows, row_threads(a.width), 0, s>>>(a);
-    }
+    cudaError_t rc;
+    if (wide ? norm_go<T, WIDE<T>, 16, 256, 3>(a, n_sm, status, s, rc) : norm_go<T, 1, 16, 256, 3>(a, n_sm, status, s, rc)) return rc;
+    if (wide ? norm_go<T, WIDE<T>, 16, 1024, 1>(a, n_sm, status, s, rc) : norm_go<T, 1, 16, 1024, 1>(a, n_sm, status, s, rc)) return rc;
+    if (wide) norm_long_kernel<T, WIDE<T>><<<(unsigned)a.rows, row_threads(a.width / WIDE<T>), 0, s>>>(a);
+    else norm_long_kernel<T, 1><<<(unsigned)a.rows, row_threads(a.width), 0, s>>>(a);
     return FEDHE_LAUNCHED();
 }
 
-template <class T, int V, bool SAMPLES>
-cudaError_t norm_grad_go(const NormGradArgs &a, const RowPlan &plan, int n_sm, cudaStream_t s) {
+template <class T, int V, int HELD, bool SAMPLES>
+bool norm_grad_go(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
+    RowPlan plan;
+    const size_t t = ((a.width + HELD - 1) / HELD + 31) / 32 * 32;
+    if (t > BACK_THREADS) return false;
+    const size_t plane = (BACK_THREADS / t) * 2 * a.width * sizeof(float), kept = SAMPLES ? (2 * plane + 15) / 16 * 16 : 0;
+    if (!plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, SHARED - 4096 - kept, plan)) return false;
+    const auto kernel = norm_grad_kernel<T, V, HELD, SAMPLES>;
+    const size_t copies = (size_t)plan.groups * plan.depth * 2 * plan.room, bytes = kept + (copies > plane ? copies : plane);
     const RunsOut out{static_cast<float *>(a.work), sum_runs(a.rows, n_sm), a.width, 2};
-    const size_t bytes = (size_t)(SAMPLES ? 3 : 1) * plan.groups * 2 * a.width * sizeof(float);
-    cudaError_t rc = cudaFuncSetAttribute(norm_grad_kernel<T, V, SAMPLES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (rc != cudaSuccess) return rc;
-    norm_grad_kernel<T, V, SAMPLES><<<out.runs, BACK_THREADS, bytes, s>>>(a, plan, out);
+    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (rc != cudaSuccess) return true;
+    kernel<<<out.runs, BACK_THREADS, bytes, s>>>(a, plan, out, status);
     rc = FEDHE_LAUNCHED();
-    return rc != cudaSuccess ? rc : join_runs(out, SAMPLES, false, a.dweight, a.dbias, s);
+    if (rc == cudaSuccess) rc = join_runs(out, SAMPLES, false, a.dweight, a.dbias, s);
+    return true;
+}
+
+template <class T, int V>
+bool norm_grad_held(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
+    if (a.over == SumOver::SAMPLES) return norm_grad_go<T, V, 8, true>(a, n_sm, status, s, rc) || norm_grad_go<T, V, 16, true>(a, n_sm, status, s, rc);
+    return norm_grad_go<T, V, 8, false>(a, n_sm, status, s, rc) || norm_grad_go<T, V, 16, false>(a, n_sm, status, s, rc);
 }
 
 template <class T>
-cudaError_t norm_grad_of(const NormGradArgs &a, int n_sm, cudaStream_t s) {
+cudaError_t norm_grad_of(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s) {
     const bool wide = wide_rows<T>(a.x.p, a.x.stride, a.width) && wide_rows<T>(a.dy.p, a.dy.stride, a.width) &&
                       wide_rows<T>(a.dx.p, a.dx.stride, a.width);
-    RowPlan plan;
-    if (plan_row(a.width, BACK_THREADS, plan)) {
-        if (a.over == SumOver::SAMPLES) return wide ? norm_grad_go<T, WIDE<T>, true>(a, plan, n_sm, s) : norm_grad_go<T, 1, true>(a, plan, n_sm, s);
-        return wide ? norm_grad_go<T, WIDE<T>, false>(a, plan, n_sm, s) : norm_grad_go<T, 1, false>(a, plan, n_sm, s);
-    }
+    cudaError_t rc;
+    if (a.rows && (wide ? norm_grad_held<T, WIDE<T>>(a, n_sm, status, s, rc) : norm_grad_held<T, 1>(a, n_sm, status, s, rc))) return rc;
     if (a.rows) {
         if (wide) norm_long_grad_kernel<T, WIDE<T>><<<(unsigned)a.rows, row_threads(a.width / WIDE<T>), 0, s>>>(a);
         else norm_long_grad_kernel<T, 1><<<(unsigned)a.rows, row_threads(a.width), 0, s>>>(a);
-        const cudaError_t rc = FEDHE_LAUNCHED();
+        rc = FEDHE_LAUNCHED();
         if (rc != cudaSuccess) return rc;
     }
     return sums<T, true>(a.dy, a.x, a.mean, a.rstd, a.rows, a.width, a.over, a.offsets, a.samples, false, a.dweight, a.dbias, a.work, n_sm, s);
@@ -599,16 +751,18 @@ cudaError_t norm_grad_of(const NormGradArgs &a, int n_sm, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, cudaStream_t s) {
-    return dtype == HE_F32 ? norm_of<float>(a, n_sm, s) : dtype == HE_BF16 ? norm_of<__nv_bfloat16>(a, n_sm, s) : norm_of<__half>(a, n_sm, s);
+cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, int *status, cudaStream_t s) {
+    return dtype == HE_F32    ? norm_of<float>(a, n_sm, status, s)
+           : dtype == HE_BF16 ? norm_of<__nv_bfloat16>(a, n_sm, status, s)
+                              : norm_of<__half>(a, n_sm, status, s);
 }
 
 size_t norm_grad_work_bytes(size_t rows, size_t width, int n_sm) { return runs_bytes(rows, width, 2, n_sm); }
 
-cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, cudaStream_t s) {
-    return dtype == HE_F32    ? norm_grad_of<float>(a, n_sm, s)
-           : dtype == HE_BF16 ? norm_grad_of<__nv_bfloat16>(a, n_sm, s)
-                              : norm_grad_of<__half>(a, n_sm, s);
+cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, int *status, cudaStream_t s) {
+    return dtype == HE_F32    ? norm_grad_of<float>(a, n_sm, status, s)
+           : dtype == HE_BF16 ? norm_grad_of<__nv_bfloat16>(a, n_sm, status, s)
+                              : norm_grad_of<__half>(a, n_sm, status, s);
 }
 
 size_t column_sums_work_bytes(size_t rows, size_t width, int n_sm) { return runs_bytes(rows, width, 1, n_sm); }
