@@ -58,6 +58,38 @@ __device__ __forceinline__ float warp_sum(float v) {
     return v;
 }
 
+// Two fp32 values that one instruction works on.
+struct F2 {
+    unsigned long long v;
+    F2() = default;
+    __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ explicit F2(float a) : F2(a, a) {}
+    __device__ __forceinline__ float2 both() const {
+        float2 r;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+        return r;
+    }
+    __device__ __forceinline__ float sum() const {
+        const float2 r = both();
+        return r.x + r.y;
+    }
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
 // The larger one; NaN where one of them is.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;

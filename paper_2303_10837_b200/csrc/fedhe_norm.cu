@@ -196,8 +196,8 @@ struct Rows {
     // A thread's packs of a row that has been copied; zeros behind its end.  A matrix's first and last bytes that no copy brings come from where they are.
     template <int V, int K>
     __device__ __forceinline__ void get(Pack<T, V> (&v)[K], size_t r, const uint8_t *room, uint32_t t, uint32_t threads, uint32_t width) const {
-        const T *row = reinterpret_cast<const T *>(room + (at(r) & 15));
-        const bool whole = from(r) <= at(r) && from(r) + size(r) >= at(r) + bytes;
+        const T *row = reinterpret_cast<const T *>(V > 1 ? room : room + (at(r) & 15));
+        const bool whole = V > 1 || (from(r) <= at(r) && from(r) + size(r) >= at(r) + bytes);
 #pragma unroll
         for (int k = 0; k < K; k++) {
             const uint32_t c = (k * threads + t) * V;
@@ -240,28 +240,38 @@ __device__ __noinline__ void copies_lost(int *status) {
     for (int i = 0; i < 20; i++) __nanosleep(1000000);
 }
 
+// A thread's elements, two and two: element e of pack k is the (k V + e) % 2 one of pair (k V + e) / 2.
 template <int V, int K>
-__device__ __forceinline__ void load_weights(float (&w)[K][V], const void *p, int type, float otherwise, uint32_t t, uint32_t threads, uint32_t width) {
+__device__ __forceinline__ void load_weights(F2 (&w)[K * V / 2], const void *p, int type, float otherwise, uint32_t t, uint32_t threads, uint32_t width) {
+    float v[K * V];
 #pragma unroll
-    for (int k = 0; k < K; k++)
-#pragma unroll
-        for (int e = 0; e < V; e++) {
-            const uint32_t c = (k * threads + t) * V + e;
-            w[k][e] = p && c < width ? load_weight(p, type, c) : otherwise;
-        }
-}
-
-// Mean and sum of squared differences from it of `n` values; two of them join to that of all (Chan, Golub and LeVeque's formula), so that
-// threads need to meet once for a row, and nothing is lost where the mean is large.
-struct Spread {
-    float n, mean, m2;
-    __device__ __forceinline__ void join(float on, float om, float o2) {
-        const float all = n + on, share = n > 0.0f ? __fdividef(on, all) : 1.0f, d = om - mean;
-        m2 += o2 + d * d * n * share;
-        mean = n > 0.0f ? fmaf(d, share, mean) : om;
-        n = all;
+    for (int i = 0; i < K * V; i++) {
+        const uint32_t c = (i / V * threads + t) * V + i % V;
+        v[i] = p && c < width ? load_weight(p, type, c) : otherwise;
     }
-};
+#pragma unroll
+    for (int i = 0; i < K * V; i += 2) w[i / 2] = F2(v[i], v[i + 1]);
+}
+template <class T, int V, int K>
+__device__ __forceinline__ void pairs_of(F2 (&x)[K * V / 2], const Pack<T, V> (&p)[K]) {
+#pragma unroll
+    for (int i = 0; i < K * V; i += 2) x[i / 2] = F2(to_f32(p[i / V].v[i % V]), to_f32(p[(i + 1) / V].v[(i + 1) % V]));
+}
+template <class T, int V, int K>
+__device__ __forceinline__ void store_row(T *row, const F2 (&x)[K * V / 2], uint32_t t, uint32_t threads, uint32_t width) {
+    Pack<T, V> o[K];
+#pragma unroll
+    for (int i = 0; i < K * V; i += 2) {
+        const float2 v = x[i / 2].both();
+        o[i / V].v[i % V] = from_f32<T>(v.x);
+        o[(i + 1) / V].v[(i + 1) % V] = from_f32<T>(v.y);
+    }
+#pragma unroll
+    for (int k = 0; k < K; k++) {
+        const uint32_t c = (k * threads + t) * V;
+        if (c < width) store_pack<T, V>(row + c, o[k]);
+    }
+}
 
 // Groups of threads take rows in turn; the weights stay in registers.
 template <class T, int V, int HELD, int THREADS, int BLOCKS>
@@ -269,7 +279,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
     constexpr int K = HELD / V;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ uint64_t bars[THREADS / 32][MOST_DEPTH];
-    __shared__ Spread met[2][THREADS / 32];
+    __shared__ float2 met[2][THREADS / 32];
+    __shared__ float counts[THREADS / 32];
     const uint32_t group = threadIdx.x / plan.threads, t = threadIdx.x % plan.threads, width = (uint32_t)a.width, lane = t & 31u;
     if (group >= plan.groups) return;
     const size_t step = (size_t)gridDim.x * plan.groups, first = (size_t)blockIdx.x * plan.groups + group;
@@ -283,65 +294,71 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
             rows.copy(first + d * step, mine + d * plan.room, &bars[group][d]);
         }
     }
-    float w[K][V], b[K][V];
+    F2 w[HELD / 2], b[HELD / 2];
     load_weights<V, K>(w, a.weight, a.weight_type, 1.0f, t, plan.threads, width);
     load_weights<V, K>(b, a.bias, a.weight_type, 0.0f, t, plan.threads, width);
     uint32_t held = 0;                                       // elements of this thread
 #pragma unroll
     for (int k = 0; k < K; k++) held += (k * plan.threads + t) * V < width ? V : 0;
     const uint32_t warps = plan.threads / 32, w0 = group * warps;
+    const float held_warp = (float)__reduce_add_sync(0xffffffffu, held);
+    if (lane == 0) counts[threadIdx.x / 32] = held_warp;
     group_sync(group, plan.threads);
     uint32_t d = 0, turn = 0, odd = 0;
     bool lost = false;                                       // a copy did not come: none is waited for any more
     for (size_t r = first; r < a.rows; r += step) {
         if (!lost && !copies_done(&bars[group][d], turn)) lost = true;
-        Pack<T, V> p[K];
-        rows.get(p, r, mine + d * plan.room, t, plan.threads, width);
-        float x[K][V], sum = 0.0f;
+        F2 x[HELD / 2];
+        {
+            Pack<T, V> p[K];
+            rows.template get<V, K>(p, r, mine + d * plan.room, t, plan.threads, width);
+            pairs_of<T, V, K>(x, p);
+        }
+        // the warp's mean and squares about it; the warps' join to the row's: sum of squares + count * (difference of means)^2, so that threads meet
+        // once, and nothing is lost where the mean is large
+        F2 s = x[0];
 #pragma unroll
-        for (int k = 0; k < K; k++)
+        for (int i = 1; i < HELD / 2; i++) s = s + x[i];
+        const float mean_warp = held_warp > 0.0f ? warp_sum(s.sum()) / held_warp : 0.0f;
+        F2 q(0.0f);
 #pragma unroll
-            for (int e = 0; e < V; e++) {
-                x[k][e] = to_f32(p[k].v[e]);
-                sum += x[k][e];
+        for (int i = 0; i < HELD / 2; i++) {
+            const F2 z = x[i] + F2(-mean_warp);
+            if (V > 1) {
+                if ((i * 2 / V * plan.threads + t) * V < width) q = fma2(z, z, q);
+            } else {
+                const float2 y = z.both();
+                const F2 of((i * 2 * plan.threads + t) < width ? y.x : 0.0f, ((i * 2 + 1) * plan.threads + t) < width ? y.y : 0.0f);
+                q = fma2(of, of, q);
             }
-        Spread s{(float)held, held ? sum / (float)held : 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < K; k++)
-#pragma unroll
-            for (int e = 0; e < V; e++)
-                if ((k * plan.threads + t) * V < width) {
-                    const float q = x[k][e] - s.mean;
-                    s.m2 = fmaf(q, q, s.m2);
-                }
-#pragma unroll
-        for (int o = 16; o; o >>= 1)
-            s.join(__shfl_xor_sync(0xffffffffu, s.n, o), __shfl_xor_sync(0xffffffffu, s.mean, o), __shfl_xor_sync(0xffffffffu, s.m2, o));
-        if (lane == 0) met[odd][threadIdx.x / 32] = s;
-        group_sync(group, plan.threads);                     // and the row is in registers: its place takes another
+        }
+        const float squares = warp_sum(q.sum());
+        float mean, rstd;
+        if (warps == 1) {
+            mean = mean_warp;
+            rstd = 1.0f / sqrtf(squares / (float)width + a.eps);
+            __syncwarp();
+        } else {
+            if (lane == 0) met[odd][threadIdx.x / 32] = make_float2(mean_warp, squares);
+            group_sync(group, plan.threads);                 // and the row is in registers: its place takes another
+            float total = 0.0f, about = 0.0f;
+            for (uint32_t i = 0; i < warps; i++) total = fmaf(counts[w0 + i], met[odd][w0 + i].x, total);
+            mean = total / (float)width;
+            for (uint32_t i = 0; i < warps; i++) {
+                const float2 m = met[odd][w0 + i];
+                about += fmaf(counts[w0 + i] * (m.x - mean), m.x - mean, m.y);
+            }
+            rstd = 1.0f / sqrtf(about / (float)width + a.eps);
+        }
         if (t == 0 && r + plan.depth * step < a.rows) {
             copies_begin(&bars[group][d], rows.size(r + plan.depth * step));
             rows.copy(r + plan.depth * step, mine + d * plan.room, &bars[group][d]);
         }
-        s = lane < warps ? met[odd][w0 + lane] : Spread{0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int o = 16; o; o >>= 1)
-            s.join(__shfl_xor_sync(0xffffffffu, s.n, o), __shfl_xor_sync(0xffffffffu, s.mean, o), __shfl_xor_sync(0xffffffffu, s.m2, o));
-        // the lanes joined in different orders: the first one's result is everyone's
-        s.mean = __shfl_sync(0xffffffffu, s.mean, 0);
-        const float rstd = 1.0f / sqrtf(__shfl_sync(0xffffffffu, s.m2, 0) / (float)width + a.eps);
-        T *y = static_cast<T *>(a.y.p) + r * a.y.stride;
-#pragma unroll
-        for (int k = 0; k < K; k++) {
-            const uint32_t c = (k * plan.threads + t) * V;
-            if (c >= width) continue;
-            Pack<T, V> o;
-#pragma unroll
-            for (int e = 0; e < V; e++) o.v[e] = from_f32<T>(fmaf((x[k][e] - s.mean) * rstd, w[k][e], b[k][e]));
-            store_pack<T, V>(y + c, o);
-        }
+        for (int i = 0; i < HELD / 2; i++) x[i] = fma2((x[i] + F2(-mean)) * F2(rstd), w[i], b[i]);
+        store_row<T, V, K>(static_cast<T *>(a.y.p) + r * a.y.stride, x, t, plan.threads, width);
         if (t == 0) {
-            a.mean[r] = s.mean;
+            a.mean[r] = mean;
             a.rstd[r] = rstd;
         }
         odd ^= 1u;
@@ -368,11 +385,12 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
     uint8_t *copies = SAMPLES ? ring + (2 * plane_words * sizeof(float) + 15) / 16 * 16 : ring;
     const auto place = [&](float *of, uint32_t g, int plane) { return of + ((size_t)g * 2 + plane) * width; };
     int cut = 0;
-    float sw[K][V], sb[K][V];
+    F2 sw[HELD / 2], sb[HELD / 2];
 #pragma unroll
-    for (int k = 0; k < K; k++)
-#pragma unroll
-        for (int e = 0; e < V; e++) sw[k][e] = sb[k][e] = 0.0f;
+    for (int i = 0; i < HELD / 2; i++) sw[i] = sb[i] = F2(0.0f);
+    // element i of this thread's, and its column
+    const auto element = [](const F2 (&v)[HELD / 2], int i) { return i % 2 ? v[i / 2].both().y : v[i / 2].both().x; };
+    const auto column = [&](int i) { return (i / V * plan.threads + t) * V + i % V; };
     if (group < plan.groups) {
         const size_t begin = lo + (hi - lo) * group / plan.groups, end = lo + (hi - lo) * (group + 1) / plan.groups;
         const Rows<T> xs(a.x, a.rows, width), dys(a.dy, a.rows, width);
@@ -387,7 +405,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             for (uint32_t d = 0; d < plan.depth && begin + d < end; d++) fetch(begin + d, d);
         }
-        float w[K][V];
+        F2 w[HELD / 2];
         load_weights<V, K>(w, a.weight, a.weight_type, 1.0f, t, plan.threads, width);
         SampleWalk walk;
         walk.begin = 0;
@@ -395,22 +413,21 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
         // what is summed so far is the head, or is added to the inner part
         const auto close = [&] {
 #pragma unroll
-            for (int k = 0; k < K; k++)
-#pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const uint32_t c = (k * plan.threads + t) * V + e;
-                    if (c < width) {
-                        if (cut) {
-                            place(inners, group, 0)[c] += fabsf(sw[k][e]);
-                            place(inners, group, 1)[c] += fabsf(sb[k][e]);
-                        } else {
-                            place(heads, group, 0)[c] = sw[k][e];
-                            place(heads, group, 1)[c] = sb[k][e];
-                            place(inners, group, 0)[c] = place(inners, group, 1)[c] = 0.0f;
-                        }
+            for (int i = 0; i < HELD; i++) {
+                const uint32_t c = column(i);
+                if (c < width) {
+                    if (cut) {
+                        place(inners, group, 0)[c] += fabsf(element(sw, i));
+                        place(inners, group, 1)[c] += fabsf(element(sb, i));
+                    } else {
+                        place(heads, group, 0)[c] = element(sw, i);
+                        place(heads, group, 1)[c] = element(sb, i);
+                        place(inners, group, 0)[c] = place(inners, group, 1)[c] = 0.0f;
                     }
-                    sw[k][e] = sb[k][e] = 0.0f;
                 }
+            }
+#pragma unroll
+            for (int i = 0; i < HELD / 2; i++) sw[i] = sb[i] = F2(0.0f);
             cut = 1;
         };
         if (SAMPLES) {
@@ -430,52 +447,49 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
                 rstd_next = a.rstd[r + 1];
             }
             if (!lost && !copies_done(&bars[group][d], turn)) lost = true;
-            float x[K][V], g[K][V], s0 = 0.0f, s1 = 0.0f;
+            F2 x[HELD / 2], g[HELD / 2], q[HELD / 2], s0(0.0f), s1(0.0f);
             {
                 Pack<T, V> px[K], pg[K];
-                xs.get(px, r, mine + d * 2 * plan.room, t, plan.threads, width);
-                dys.get(pg, r, mine + (d * 2 + 1) * plan.room, t, plan.threads, width);
-#pragma unroll
-                for (int k = 0; k < K; k++)
-#pragma unroll
-                    for (int e = 0; e < V; e++) {
-                        x[k][e] = (to_f32(px[k].v[e]) - mean) * rstd;
-                        g[k][e] = to_f32(pg[k].v[e]);
-                        const float q = g[k][e] * w[k][e];   // behind the row's end g is 0
-                        s0 += q;
-                        s1 = fmaf(q, x[k][e], s1);
-                    }
+                xs.template get<V, K>(px, r, mine + d * 2 * plan.room, t, plan.threads, width);
+                dys.template get<V, K>(pg, r, mine + (d * 2 + 1) * plan.room, t, plan.threads, width);
+                pairs_of<T, V, K>(x, px);
+                pairs_of<T, V, K>(g, pg);
             }
-            s0 = warp_sum(s0);
-            s1 = warp_sum(s1);
-            if (lane == 0) met[r & 1][threadIdx.x / 32] = make_float2(s0, s1);
+#pragma unroll
+            for (int i = 0; i < HELD / 2; i++) {
+                x[i] = (x[i] + F2(-mean)) * F2(rstd);
+                q[i] = g[i] * w[i];                          // behind the row's end g is 0
+                s0 = s0 + q[i];
+                s1 = fma2(q[i], x[i], s1);
+            }
+            float ma = warp_sum(s0.sum()), man = warp_sum(s1.sum());
+            if (warps > 1 && lane == 0) met[r & 1][threadIdx.x / 32] = make_float2(ma, man);
             if (SAMPLES && (int64_t)r >= walk.end) {
                 close();
                 walk.next((int64_t)r);
             }
             if (!SAMPLES || (int64_t)r >= walk.begin) {
 #pragma unroll
-                for (int k = 0; k < K; k++)
-#pragma unroll
-                    for (int e = 0; e < V; e++) {
-                        sw[k][e] = fmaf(g[k][e], x[k][e], sw[k][e]);
-                        sb[k][e] += g[k][e];
-                    }
+                for (int i = 0; i < HELD / 2; i++) {
+                    sw[i] = fma2(g[i], x[i], sw[i]);
+                    sb[i] = sb[i] + g[i];
+                }
             }
             group_sync(group, plan.threads);                 // and the rows are in registers: their places take others
             if (t == 0 && r + plan.depth < end) fetch(r + plan.depth, d);
-            const float2 of = lane < warps ? met[r & 1][w0 + lane] : make_float2(0.0f, 0.0f);
-            const float ma = warp_sum(of.x) * n, man = warp_sum(of.y) * n;
-            T *dx = static_cast<T *>(a.dx.p) + r * a.dx.stride;
-#pragma unroll
-            for (int k = 0; k < K; k++) {
-                const uint32_t c = (k * plan.threads + t) * V;
-                if (c >= width) continue;
-                Pack<T, V> o;
-#pragma unroll
-                for (int e = 0; e < V; e++) o.v[e] = from_f32<T>(rstd * (fmaf(g[k][e], w[k][e], -ma) - x[k][e] * man));
-                store_pack<T, V>(dx + c, o);
+            if (warps > 1) {
+                ma = man = 0.0f;
+                for (uint32_t i = 0; i < warps; i++) {
+                    const float2 of = met[r & 1][w0 + i];
+                    ma += of.x;
+                    man += of.y;
+                }
             }
+            ma *= n;
+            man *= n;
+#pragma unroll
+            for (int i = 0; i < HELD / 2; i++) x[i] = F2(rstd) * fma2(x[i], F2(-man), q[i] + F2(-ma));
+            store_row<T, V, K>(static_cast<T *>(a.dx.p) + r * a.dx.stride, x, t, plan.threads, width);
             if (++d == plan.depth) d = 0, turn ^= 1u;
         }
         if (lost) copies_lost(status);
@@ -485,15 +499,13 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
         // what is left is the tail, or the head of a run without a cut
         float *to = SAMPLES && cut ? tails : heads;
 #pragma unroll
-        for (int k = 0; k < K; k++)
-#pragma unroll
-            for (int e = 0; e < V; e++) {
-                const uint32_t c = (k * plan.threads + t) * V + e;
-                if (c < width) {
-                    place(to, group, 0)[c] = sw[k][e];
-                    place(to, group, 1)[c] = sb[k][e];
-                }
+        for (int i = 0; i < HELD; i++) {
+            const uint32_t c = column(i);
+            if (c < width) {
+                place(to, group, 0)[c] = element(sw, i);
+                place(to, group, 1)[c] = element(sb, i);
             }
+        }
         if (SAMPLES && t == 0) cuts[group] = cut;
     }
     __syncthreads();
