@@ -163,71 +163,70 @@ __device__ __forceinline__ void group_sync(uint32_t group, uint32_t threads) {
     else asm volatile("barrier.sync %0, %1;" ::"r"(group + 1), "r"(threads) : "memory");
 }
 
-// The rows of a matrix as copies see them: whole 16 bytes, none outside the memory that the matrix spans.
-template <class T>
+// The rows of a matrix as copies see them: whole 16 bytes, none outside the memory that the matrix spans.  EVEN: every row begins and ends on 16
+// bytes, and nothing is left over.
+template <class T, bool EVEN>
 struct Rows {
-    const T *p;
-    size_t stride;
+    const uint8_t *p;
+    size_t pitch;                                            // bytes from row to row
     uintptr_t low, high;                                     // whole 16 bytes of the matrix
     uint32_t bytes;                                          // of a row
-    __device__ __forceinline__ Rows(const MatArg &m, size_t rows, uint32_t width) : p(static_cast<const T *>(m.p)), stride(m.stride), bytes(width * (uint32_t)sizeof(T)) {
+    __device__ __forceinline__ Rows(const MatArg &m, size_t rows, uint32_t width)
+        : p(static_cast<const uint8_t *>(m.p)), pitch(m.stride * sizeof(T)), bytes(width * (uint32_t)sizeof(T)) {
         low = (reinterpret_cast<uintptr_t>(p) + 15) & ~(uintptr_t)15;
-        high = (reinterpret_cast<uintptr_t>(p + (rows - 1) * stride) + bytes) & ~(uintptr_t)15;
+        high = (reinterpret_cast<uintptr_t>(p + (rows - 1) * pitch) + bytes) & ~(uintptr_t)15;
     }
-    __device__ __forceinline__ uintptr_t at(size_t r) const { return reinterpret_cast<uintptr_t>(p + r * stride); }
-    // what is copied of a row
-    __device__ __forceinline__ uintptr_t from(size_t r) const {
-        const uintptr_t a = at(r) & ~(uintptr_t)15;
-        return a < low ? low : a;
+    __device__ __forceinline__ uintptr_t at(size_t r) const { return reinterpret_cast<uintptr_t>(p) + r * pitch; }
+    // what is copied of the row at an address
+    __device__ __forceinline__ uintptr_t from(uintptr_t row) const {
+        const uintptr_t a = row & ~(uintptr_t)15;
+        return EVEN ? row : a < low ? low : a;
     }
-    __device__ __forceinline__ uint32_t size(size_t r) const {
-        uintptr_t e = (at(r) + bytes + 15) & ~(uintptr_t)15;
+    __device__ __forceinline__ uint32_t size(uintptr_t row) const {
+        if (EVEN) return bytes;
+        uintptr_t e = (row + bytes + 15) & ~(uintptr_t)15;
         if (e > high) e = high;
-        return e > from(r) ? (uint32_t)(e - from(r)) : 0;
+        return e > from(row) ? (uint32_t)(e - from(row)) : 0;
     }
-    __device__ __forceinline__ void copy(size_t r, uint8_t *room, uint64_t *bar) const {
-        const uint32_t n = size(r);
-        if (!n) return;
-        const uint32_t to = (uint32_t)__cvta_generic_to_shared(room) + (uint32_t)(from(r) - (at(r) & ~(uintptr_t)15));
-        asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from(r)), "r"(n),
-                     "r"((uint32_t)__cvta_generic_to_shared(bar))
-                     : "memory");
+    __device__ __forceinline__ void copy(uintptr_t row, uint32_t room, uint32_t bar) const {
+        const uint32_t n = size(row);
+        if (!EVEN && !n) return;
+        const uint32_t to = EVEN ? room : room + (uint32_t)(from(row) - (row & ~(uintptr_t)15));
+        asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from(row)), "r"(n), "r"(bar) : "memory");
     }
     // A thread's packs of a row that has been copied; zeros behind its end.  A matrix's first and last bytes that no copy brings come from where they are.
     template <int V, int K>
-    __device__ __forceinline__ void get(Pack<T, V> (&v)[K], size_t r, const uint8_t *room, uint32_t t, uint32_t threads, uint32_t width) const {
-        const T *row = reinterpret_cast<const T *>(V > 1 ? room : room + (at(r) & 15));
-        const bool whole = V > 1 || (from(r) <= at(r) && from(r) + size(r) >= at(r) + bytes);
+    __device__ __forceinline__ void get(Pack<T, V> (&v)[K], uintptr_t row, const uint8_t *room, uint32_t t, uint32_t threads, uint32_t width) const {
+        const T *in = reinterpret_cast<const T *>(EVEN ? room : room + (row & 15)) + t * V;
 #pragma unroll
         for (int k = 0; k < K; k++) {
-            const uint32_t c = (k * threads + t) * V;
-            if (c < width) v[k] = load_pack<T, V>(row + c);
+            if ((k * threads + t) * V < width) v[k] = load_pack<T, V>(in + k * threads * V);
             else
 #pragma unroll
                 for (int e = 0; e < V; e++) v[k].v[e] = from_f32<T>(0.0f);
         }
-        if (!whole)
+        if (!EVEN && (row < low || row + bytes > high)) {
 #pragma unroll
-            for (int k = 0; k < K; k++)
-#pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const uint32_t c = (k * threads + t) * V + e;
-                    const uintptr_t x = at(r) + c * sizeof(T);
-                    if (c < width && (x < from(r) || x >= from(r) + size(r))) v[k].v[e] = p[r * stride + c];
-                }
+            for (int i = 0; i < K * V; i++) {
+                const uint32_t c = (i / V * threads + t) * V + i % V;
+                const uintptr_t x = row + c * sizeof(T);
+                if (c < width && (x < from(row) || x >= from(row) + size(row))) v[i / V].v[i % V] = *reinterpret_cast<const T *>(x);
+            }
+        }
     }
 };
 
-__device__ __forceinline__ void copies_begin(uint64_t *bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"((uint32_t)__cvta_generic_to_shared(bar)), "r"(bytes) : "memory");
+__device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copies_begin(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 constexpr uint32_t COPY_TRIES = 256;             // of 10 ms at most
-__device__ __forceinline__ bool copies_done(uint64_t *bar, uint32_t parity) {
+__device__ __forceinline__ bool copies_done(uint32_t bar, uint32_t parity) {
     for (uint32_t i = 0; i < COPY_TRIES; i++) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done)
-                     : "r"((uint32_t)__cvta_generic_to_shared(bar)), "r"(parity)
+                     : "r"(bar), "r"(parity)
                      : "memory");
         if (done) return true;
     }
@@ -238,6 +237,18 @@ __device__ __forceinline__ bool copies_done(uint64_t *bar, uint32_t parity) {
 __device__ __noinline__ void copies_lost(int *status) {
     atomicOr(status, STATUS_COPY);
     for (int i = 0; i < 20; i++) __nanosleep(1000000);
+}
+
+// The sum over the first `lanes` lanes (a power of two; the others hold the same again); the same bits in every lane.
+__device__ __forceinline__ float few_sum(float v, uint32_t lanes) {
+    for (uint32_t o = lanes / 2; o; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ uint32_t power_above(uint32_t n) { return n <= 1 ? 1 : 2u << (31 - __clz((int)(n - 1))); }
+// 1 / sqrt(v): rsqrtf and a step of Newton's iteration
+__device__ __forceinline__ float inverse_root(float v) {
+    const float r = rsqrtf(v);
+    return v > 0.0f && r > 0.0f ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
 // A thread's elements, two and two: element e of pack k is the (k V + e) % 2 one of pair (k V + e) / 2.
@@ -283,16 +294,24 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
     __shared__ float counts[THREADS / 32];
     const uint32_t group = threadIdx.x / plan.threads, t = threadIdx.x % plan.threads, width = (uint32_t)a.width, lane = t & 31u;
     if (group >= plan.groups) return;
-    const size_t step = (size_t)gridDim.x * plan.groups, first = (size_t)blockIdx.x * plan.groups + group;
-    const Rows<T> rows(a.x, a.rows, width);
+    const uint32_t step = gridDim.x * plan.groups, first = blockIdx.x * plan.groups + group, count = (uint32_t)a.rows;
+    const Rows<T, (V > 1)> rows(a.x, a.rows, width);
     uint8_t *mine = ring + (size_t)group * plan.depth * plan.room;
+    const uint32_t mine_at = shared_at(mine), bar = shared_at(&bars[group][0]);
+    uint32_t asked = first;                                  // by the group's first thread: the next row to copy, and where it is
+    uintptr_t asked_at = rows.at(first);
+    const uintptr_t stride = (uintptr_t)step * rows.pitch;
+    const auto ask = [&](uint32_t d) {
+        if (asked >= count) return;
+        copies_begin(bar + d * 8, rows.size(asked_at));
+        rows.copy(asked_at, mine_at + d * plan.room, bar + d * 8);
+        asked += step;
+        asked_at += stride;
+    };
     if (t == 0) {
-        for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bars[group][d])) : "memory");
+        for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + d * 8) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (uint32_t d = 0; d < plan.depth && first + d * step < a.rows; d++) {
-            copies_begin(&bars[group][d], rows.size(first + d * step));
-            rows.copy(first + d * step, mine + d * plan.room, &bars[group][d]);
-        }
+        for (uint32_t d = 0; d < plan.depth; d++) ask(d);
     }
     F2 w[HELD / 2], b[HELD / 2];
     load_weights<V, K>(w, a.weight, a.weight_type, 1.0f, t, plan.threads, width);
@@ -300,67 +319,64 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
     uint32_t held = 0;                                       // elements of this thread
 #pragma unroll
     for (int k = 0; k < K; k++) held += (k * plan.threads + t) * V < width ? V : 0;
-    const uint32_t warps = plan.threads / 32, w0 = group * warps;
-    const float held_warp = (float)__reduce_add_sync(0xffffffffu, held);
+    const uint32_t warps = plan.threads / 32, w0 = group * warps, lanes = power_above(warps), other = lane % lanes;
+    const float held_warp = (float)__reduce_add_sync(0xffffffffu, held), part = held_warp > 0.0f ? 1.0f / held_warp : 0.0f;
     if (lane == 0) counts[threadIdx.x / 32] = held_warp;
     group_sync(group, plan.threads);
+    const float count_other = other < warps ? counts[w0 + other] : 0.0f, part_other = count_other > 0.0f ? 1.0f / count_other : 0.0f;
     uint32_t d = 0, turn = 0, odd = 0;
+    uintptr_t row = rows.at(first);
+    T *y = static_cast<T *>(a.y.p) + (size_t)first * a.y.stride;
     bool lost = false;                                       // a copy did not come: none is waited for any more
-    for (size_t r = first; r < a.rows; r += step) {
-        if (!lost && !copies_done(&bars[group][d], turn)) lost = true;
+    for (uint32_t r = first; r < count; r += step) {
+        if (!lost && !copies_done(bar + d * 8, turn)) lost = true;
         F2 x[HELD / 2];
         {
             Pack<T, V> p[K];
-            rows.template get<V, K>(p, r, mine + d * plan.room, t, plan.threads, width);
+            rows.template get<V, K>(p, row, mine + d * plan.room, t, plan.threads, width);
             pairs_of<T, V, K>(x, p);
         }
-        // the warp's mean and squares about it; the warps' join to the row's: sum of squares + count * (difference of means)^2, so that threads meet
-        // once, and nothing is lost where the mean is large
+        // The warp's sum, and squares about what is its mean but for a rounding; the warps' join to the row's squares: sum of squares + count *
+        // (difference of means)^2.  So threads meet once, and nothing is lost where the mean is large.
         F2 s = x[0];
 #pragma unroll
         for (int i = 1; i < HELD / 2; i++) s = s + x[i];
-        const float mean_warp = held_warp > 0.0f ? warp_sum(s.sum()) / held_warp : 0.0f;
+        const float sum = warp_sum(s.sum()), about = sum * part;
         F2 q(0.0f);
 #pragma unroll
         for (int i = 0; i < HELD / 2; i++) {
-            const F2 z = x[i] + F2(-mean_warp);
+            const F2 z = x[i] + F2(-about);
             if (V > 1) {
                 if ((i * 2 / V * plan.threads + t) * V < width) q = fma2(z, z, q);
             } else {
-                const float2 y = z.both();
-                const F2 of((i * 2 * plan.threads + t) < width ? y.x : 0.0f, ((i * 2 + 1) * plan.threads + t) < width ? y.y : 0.0f);
+                const float2 y2 = z.both();
+                const F2 of((i * 2 * plan.threads + t) < width ? y2.x : 0.0f, ((i * 2 + 1) * plan.threads + t) < width ? y2.y : 0.0f);
                 q = fma2(of, of, q);
             }
         }
-        const float squares = warp_sum(q.sum());
-        float mean, rstd;
+        float squares = warp_sum(q.sum()), mean;
         if (warps == 1) {
-            mean = mean_warp;
-            rstd = 1.0f / sqrtf(squares / (float)width + a.eps);
+            mean = sum / (float)width;
             __syncwarp();
         } else {
-            if (lane == 0) met[odd][threadIdx.x / 32] = make_float2(mean_warp, squares);
+            if (lane == 0) met[odd][threadIdx.x / 32] = make_float2(sum, squares);
             group_sync(group, plan.threads);                 // and the row is in registers: its place takes another
-            float total = 0.0f, about = 0.0f;
-            for (uint32_t i = 0; i < warps; i++) total = fmaf(counts[w0 + i], met[odd][w0 + i].x, total);
-            mean = total / (float)width;
-            for (uint32_t i = 0; i < warps; i++) {
-                const float2 m = met[odd][w0 + i];
-                about += fmaf(counts[w0 + i] * (m.x - mean), m.x - mean, m.y);
-            }
-            rstd = 1.0f / sqrtf(about / (float)width + a.eps);
+            const float2 m = other < warps ? met[odd][w0 + other] : make_float2(0.0f, 0.0f);
+            mean = few_sum(m.x, lanes) / (float)width;
+            const float off = m.x * part_other - mean;
+            squares = few_sum(fmaf(count_other * off, off, m.y), lanes);
         }
-        if (t == 0 && r + plan.depth * step < a.rows) {
-            copies_begin(&bars[group][d], rows.size(r + plan.depth * step));
-            rows.copy(r + plan.depth * step, mine + d * plan.room, &bars[group][d]);
-        }
-#pragma unroll
-        for (int i = 0; i < HELD / 2; i++) x[i] = fma2((x[i] + F2(-mean)) * F2(rstd), w[i], b[i]);
-        store_row<T, V, K>(static_cast<T *>(a.y.p) + r * a.y.stride, x, t, plan.threads, width);
+        const float rstd = inverse_root(squares / (float)width + a.eps);
         if (t == 0) {
+            ask(d);
             a.mean[r] = mean;
             a.rstd[r] = rstd;
         }
+#pragma unroll
+        for (int i = 0; i < HELD / 2; i++) x[i] = fma2((x[i] + F2(-mean)) * F2(rstd), w[i], b[i]);
+        store_row<T, V, K>(y, x, t, plan.threads, width);
+        y += step * a.y.stride;
+        row += stride;
         odd ^= 1u;
         if (++d == plan.depth) d = 0, turn ^= 1u;
     }
@@ -392,18 +408,25 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
     const auto element = [](const F2 (&v)[HELD / 2], int i) { return i % 2 ? v[i / 2].both().y : v[i / 2].both().x; };
     const auto column = [&](int i) { return (i / V * plan.threads + t) * V + i % V; };
     if (group < plan.groups) {
-        const size_t begin = lo + (hi - lo) * group / plan.groups, end = lo + (hi - lo) * (group + 1) / plan.groups;
-        const Rows<T> xs(a.x, a.rows, width), dys(a.dy, a.rows, width);
+        const uint32_t begin = (uint32_t)(lo + (hi - lo) * group / plan.groups), end = (uint32_t)(lo + (hi - lo) * (group + 1) / plan.groups);
+        const Rows<T, (V > 1)> xs(a.x, a.rows, width), dys(a.dy, a.rows, width);
         uint8_t *mine = copies + (size_t)group * plan.depth * 2 * plan.room;
-        const auto fetch = [&](size_t r, uint32_t d) {
-            copies_begin(&bars[group][d], xs.size(r) + dys.size(r));
-            xs.copy(r, mine + d * 2 * plan.room, &bars[group][d]);
-            dys.copy(r, mine + (d * 2 + 1) * plan.room, &bars[group][d]);
+        const uint32_t mine_at = shared_at(mine), bar = shared_at(&bars[group][0]);
+        uint32_t asked = begin;                              // by the group's first thread: the next rows to copy, and where they are
+        uintptr_t x_asked = xs.at(begin), dy_asked = dys.at(begin);
+        const auto ask = [&](uint32_t d) {
+            if (asked >= end) return;
+            copies_begin(bar + d * 8, xs.size(x_asked) + dys.size(dy_asked));
+            xs.copy(x_asked, mine_at + d * 2 * plan.room, bar + d * 8);
+            dys.copy(dy_asked, mine_at + (d * 2 + 1) * plan.room, bar + d * 8);
+            asked++;
+            x_asked += xs.pitch;
+            dy_asked += dys.pitch;
         };
         if (t == 0) {
-            for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"((uint32_t)__cvta_generic_to_shared(&bars[group][d])) : "memory");
+            for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + d * 8) : "memory");
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            for (uint32_t d = 0; d < plan.depth && begin + d < end; d++) fetch(begin + d, d);
+            for (uint32_t d = 0; d < plan.depth; d++) ask(d);
         }
         F2 w[HELD / 2];
         load_weights<V, K>(w, a.weight, a.weight_type, 1.0f, t, plan.threads, width);
@@ -434,24 +457,26 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
             walk.seek(a.offsets, a.samples, (int64_t)begin);
             if (walk.begin == (int64_t)begin) close();       // the run before this one ends with another sample
         }
-        const uint32_t warps = plan.threads / 32, w0 = group * warps;
+        const uint32_t warps = plan.threads / 32, w0 = group * warps, lanes = power_above(warps), other = lane % lanes;
         const float n = 1.0f / (float)width;
         float mean_next = begin < end ? a.mean[begin] : 0.0f, rstd_next = begin < end ? a.rstd[begin] : 0.0f;
         group_sync(group, plan.threads);
         uint32_t d = 0, turn = 0;
+        uintptr_t x_row = xs.at(begin), dy_row = dys.at(begin);
+        T *dx = static_cast<T *>(a.dx.p) + (size_t)begin * a.dx.stride;
         bool lost = false;
-        for (size_t r = begin; r < end; r++) {
+        for (uint32_t r = begin; r < end; r++) {
             const float mean = mean_next, rstd = rstd_next;
             if (r + 1 < end) {
                 mean_next = a.mean[r + 1];
                 rstd_next = a.rstd[r + 1];
             }
-            if (!lost && !copies_done(&bars[group][d], turn)) lost = true;
+            if (!lost && !copies_done(bar + d * 8, turn)) lost = true;
             F2 x[HELD / 2], g[HELD / 2], q[HELD / 2], s0(0.0f), s1(0.0f);
             {
                 Pack<T, V> px[K], pg[K];
-                xs.template get<V, K>(px, r, mine + d * 2 * plan.room, t, plan.threads, width);
-                dys.template get<V, K>(pg, r, mine + (d * 2 + 1) * plan.room, t, plan.threads, width);
+                xs.template get<V, K>(px, x_row, mine + d * 2 * plan.room, t, plan.threads, width);
+                dys.template get<V, K>(pg, dy_row, mine + (d * 2 + 1) * plan.room, t, plan.threads, width);
                 pairs_of<T, V, K>(x, px);
                 pairs_of<T, V, K>(g, pg);
             }
@@ -476,20 +501,20 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
                 }
             }
             group_sync(group, plan.threads);                 // and the rows are in registers: their places take others
-            if (t == 0 && r + plan.depth < end) fetch(r + plan.depth, d);
+            if (t == 0) ask(d);
             if (warps > 1) {
-                ma = man = 0.0f;
-                for (uint32_t i = 0; i < warps; i++) {
-                    const float2 of = met[r & 1][w0 + i];
-                    ma += of.x;
-                    man += of.y;
-                }
+                const float2 m = other < warps ? met[r & 1][w0 + other] : make_float2(0.0f, 0.0f);
+                ma = few_sum(m.x, lanes);
+                man = few_sum(m.y, lanes);
             }
             ma *= n;
             man *= n;
 #pragma unroll
             for (int i = 0; i < HELD / 2; i++) x[i] = F2(rstd) * fma2(x[i], F2(-man), q[i] + F2(-ma));
-            store_row<T, V, K>(static_cast<T *>(a.dx.p) + r * a.dx.stride, x, t, plan.threads, width);
+            store_row<T, V, K>(dx, x, t, plan.threads, width);
+            dx += a.dx.stride;
+            x_row += xs.pitch;
+            dy_row += dys.pitch;
             if (++d == plan.depth) d = 0, turn ^= 1u;
         }
         if (lost) copies_lost(status);
@@ -723,12 +748,12 @@ cudaError_t norm_of(const NormArgs &a, int n_sm, int *status, cudaStream_t s) {
 }
 
 template <class T, int V, int HELD, bool SAMPLES>
-bool norm_grad_go(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
+bool norm_grad_go(const NormGradArgs &a, uint32_t depth, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
     RowPlan plan;
     const size_t t = ((a.width + HELD - 1) / HELD + 31) / 32 * 32;
     if (t > BACK_THREADS) return false;
     const size_t plane = (BACK_THREADS / t) * 2 * a.width * sizeof(float), kept = SAMPLES ? (2 * plane + 15) / 16 * 16 : 0;
-    if (!plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, SHARED - 4096 - kept, plan)) return false;
+    if (kept > SHARED - 4096 || !plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, SHARED - 4096 - kept, plan) || plan.depth < depth) return false;
     const auto kernel = norm_grad_kernel<T, V, HELD, SAMPLES>;
     const size_t copies = (size_t)plan.groups * plan.depth * 2 * plan.room, bytes = kept + (copies > plane ? copies : plane);
     const RunsOut out{static_cast<float *>(a.work), sum_runs(a.rows, n_sm), a.width, 2};
@@ -742,8 +767,8 @@ bool norm_grad_go(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, 
 
 template <class T, int V>
 bool norm_grad_held(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
-    if (a.over == SumOver::SAMPLES) return norm_grad_go<T, V, 8, true>(a, n_sm, status, s, rc) || norm_grad_go<T, V, 16, true>(a, n_sm, status, s, rc);
-    return norm_grad_go<T, V, 8, false>(a, n_sm, status, s, rc) || norm_grad_go<T, V, 16, false>(a, n_sm, status, s, rc);
+    if (a.over == SumOver::SAMPLES) return norm_grad_go<T, V, 16, true>(a, 2, n_sm, status, s, rc) || norm_grad_go<T, V, 8, true>(a, 2, n_sm, status, s, rc) || norm_grad_go<T, V, 16, true>(a, 1, n_sm, status, s, rc);
+    return norm_grad_go<T, V, 16, false>(a, 1, n_sm, status, s, rc);
 }
 
 template <class T>
