@@ -245,6 +245,11 @@ __device__ __forceinline__ float few_sum(float v, uint32_t lanes) {
     return v;
 }
 __device__ __forceinline__ uint32_t power_above(uint32_t n) { return n <= 1 ? 1 : 2u << (31 - __clz((int)(n - 1))); }
+// sum / n, given 1 / n rounded: the product and what is left over.  Exact where the quotient is.
+__device__ __forceinline__ float quotient(float sum, float n, float part) {
+    const float q = sum * part;
+    return fmaf(fmaf(-q, n, sum), part, q);
+}
 // 1 / sqrt(v): rsqrtf and a step of Newton's iteration
 __device__ __forceinline__ float inverse_root(float v) {
     const float r = rsqrtf(v);
@@ -324,6 +329,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
     if (lane == 0) counts[threadIdx.x / 32] = held_warp;
     group_sync(group, plan.threads);
     const float count_other = other < warps ? counts[w0 + other] : 0.0f, part_other = count_other > 0.0f ? 1.0f / count_other : 0.0f;
+    const float all = (float)width, part_all = 1.0f / all;
     uint32_t d = 0, turn = 0, odd = 0;
     uintptr_t row = rows.at(first);
     T *y = static_cast<T *>(a.y.p) + (size_t)first * a.y.stride;
@@ -356,17 +362,17 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
         }
         float squares = warp_sum(q.sum()), mean;
         if (warps == 1) {
-            mean = sum / (float)width;
+            mean = quotient(sum, all, part_all);
             __syncwarp();
         } else {
             if (lane == 0) met[odd][threadIdx.x / 32] = make_float2(sum, squares);
             group_sync(group, plan.threads);                 // and the row is in registers: its place takes another
             const float2 m = other < warps ? met[odd][w0 + other] : make_float2(0.0f, 0.0f);
-            mean = few_sum(m.x, lanes) / (float)width;
+            mean = quotient(few_sum(m.x, lanes), all, part_all);
             const float off = m.x * part_other - mean;
             squares = few_sum(fmaf(count_other * off, off, m.y), lanes);
         }
-        const float rstd = inverse_root(squares / (float)width + a.eps);
+        const float rstd = inverse_root(fmaf(squares, part_all, a.eps));
         if (t == 0) {
             ask(d);
             a.mean[r] = mean;
