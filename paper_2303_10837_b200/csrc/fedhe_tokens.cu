@@ -25,30 +25,36 @@ __device__ __forceinline__ float ex2(float x) {
     return r;
 }
 
-// Maximum, sum of 2^t and sum of t 2^t over t = (z - maximum) log2 e.  All in fp32: sums of up to 2^31 terms that are at most 1, as
-// partial sums of the threads.
+// Maximum, sum of 2^t and sum of t 2^t over t = (z - maximum) log2 e, two sums side by side.  All in fp32: sums of up to 2^31 terms that are
+// at most 1, as partial sums of the threads.
 struct Soft {
-    float m, s, w;
+    float m;
+    F2 s, w;
     __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.0f : m; }
     __device__ __forceinline__ void rise(float to) {         // to a larger maximum
         const float b = to == -INFINITY ? 0.0f : to, d = max_nan((m - b) * LOG2E, FAR), f = ex2(d);
-        w = f * (w + s * d);
-        s *= f;
+        w = F2(f) * fma2(s, F2(d), w);
+        s = s * F2(f);
         m = to;
     }
-    __device__ __forceinline__ void add(float z, float b) {
-        const float t = max_nan((z - b) * LOG2E, FAR), e = ex2(t);
-        s += e;
-        w = fmaf(e, t, w);
+    __device__ __forceinline__ void add(F2 z, float b) {
+        const float2 t = ((z + F2(-b)) * F2(LOG2E)).both();
+        const F2 u(max_nan(t.x, FAR), max_nan(t.y, FAR)), e(ex2(max_nan(t.x, FAR)), ex2(max_nan(t.y, FAR)));
+        s = s + e;
+        w = fma2(e, u, w);
     }
     __device__ __forceinline__ void join(Soft o) {
         const float to = fmaxf(m, o.m);
         rise(to);
         o.rise(to);
-        s += o.s;
-        w += o.w;
+        s = s + o.s;
+        w = w + o.w;
     }
 };
+__device__ __forceinline__ Soft far(const Soft &q, int o) {       // another lane's, its two sums as one
+    const float s = q.s.sum(), w = q.w.sum();
+    return Soft{__shfl_xor_sync(0xffffffffu, q.m, o), F2(__shfl_xor_sync(0xffffffffu, s, o), 0.0f), F2(__shfl_xor_sync(0xffffffffu, w, o), 0.0f)};
+}
 
 // Order of the alternatives: the value, NaN as low as -inf, then the lowest index.
 __device__ __forceinline__ uint32_t order_of(float z) {
@@ -59,6 +65,19 @@ __device__ __forceinline__ uint32_t order_of(float z) {
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
 __device__ __forceinline__ uint64_t key_of(float z, uint32_t index) { return (uint64_t)order_of(z) << 32 | (0xffffffffu - index); }
 
+// A row's first or last vector, by its elements.
+template <class T>
+__device__ __noinline__ uint4 load_end(const T *p, int64_t first, uint32_t n) {
+    Pack<T, WIDE<T>> a;
+#pragma unroll
+    for (int e = 0; e < WIDE<T>; e++) {
+        const int64_t i = first + e;
+        a.v[e] = i >= 0 && i < (int64_t)n ? p[i] : from_f32<T>(-INFINITY);
+    }
+    uint4 w;
+    memcpy(&w, &a, 16);
+    return w;
+}
 // A row as aligned vectors: vector v holds the elements v * V - shift, .... The first and the last may reach outside; those elements
 // are not read.
 template <class T>
@@ -74,15 +93,32 @@ struct Row {
     __device__ __forceinline__ bool whole(uint32_t v) const { return first(v) >= 0 && first(v) + V <= n; }
     __device__ __forceinline__ Pack<T, V> load(uint32_t v) const {
         if (v < vectors && whole(v)) return load_pack<T, V>(p + first(v));
+        const uint4 w = load_end<T>(p, first(v), n);
         Pack<T, V> a;
-#pragma unroll
-        for (int e = 0; e < V; e++) {
-            const int64_t i = first(v) + e;
-            a.v[e] = i >= 0 && i < (int64_t)n ? p[i] : from_f32<T>(-INFINITY);
-        }
+        memcpy(&a, &w, 16);
         return a;
     }
 };
+
+template <class T>
+__device__ __forceinline__ float top_of(const Pack<T, WIDE<T>> &p) {          // NaN does not count
+    float m = to_f32(p.v[0]);
+#pragma unroll
+    for (int e = 1; e < WIDE<T>; e++) m = fmaxf(m, to_f32(p.v[e]));
+    return m;
+}
+template <>
+__device__ __forceinline__ float top_of<__nv_bfloat16>(const Pack<__nv_bfloat16, 8> &p) {
+    const __nv_bfloat162 *w = reinterpret_cast<const __nv_bfloat162 *>(&p);
+    const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+template <>
+__device__ __forceinline__ float top_of<__half>(const Pack<__half, 8> &p) {
+    const __half2 *w = reinterpret_cast<const __half2 *>(&p);
+    const __half2 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
 
 struct Found {
     uint64_t key[FOUND];
@@ -96,6 +132,7 @@ __device__ __forceinline__ uint32_t keep_best(Found &f, uint32_t n, uint32_t top
     for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
         const uint64_t mine = f.key[i];
         uint32_t above = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < n; j++) above += f.key[j] > mine;
         if (above < top) f.best[above] = mine;
     }
@@ -124,144 +161,175 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
     return low;
 }
 
-// One row by a cluster of C blocks (C = 1: by a block), which take the row's pieces in turn.  A piece stays in registers while its
-// maximum, its sums and its candidates for the alternatives are found.  The candidates: values that are not below a bound on the top-th value,
-// in shared memory, of which the best are kept now and then and raise the bound.  Rows of many equal values can overflow
-// the candidates' room; a piece that does is searched once for each alternative instead.
-template <class T, bool TOP>
-__global__ void __launch_bounds__(256) log_probs_kernel(const LogProbsArgs a, const uint32_t C) {
+// The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are as high as the
+// bound that the candidates have no room.
+template <class T>
+__device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t first, uint32_t step, uint32_t pieces, uint32_t top) {
     constexpr int V = WIDE<T>, NV = ROW_ELEMENTS / V;
-    __shared__ Soft soft[8];
-    __shared__ Soft mine;
+    const uint32_t NT = blockDim.x;
+    uint64_t below = ~0ull;
+    uint32_t n = 0;
+    __syncthreads();
+    for (; n < top; n++) {
+        uint64_t best = 0;
+        for (uint32_t c = first; c < pieces; c += step)
+            for (uint32_t i = 0; i < NV; i++) {
+                const uint32_t v = (c * NV + i) * NT + threadIdx.x;
+                if (v >= row.vectors) break;
+                const Pack<T, V> p = row.load(v);
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    const int64_t j = row.first(v) + e;
+                    const uint64_t k = key_of(to_f32(p.v[e]), (uint32_t)j);
+                    if (j >= 0 && j < (int64_t)row.n && k < below && k > best) best = k;
+                }
+            }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+        if ((threadIdx.x & 31u) == 0) f.most[threadIdx.x / 32] = best;
+        __syncthreads();
+        for (uint32_t w = 0; w < NT / 32; w++) best = max(best, f.most[w]);
+        __syncthreads();
+        if (best == 0) break;                // a key of an element is not 0: its index is below 2^32 - 1
+        if (threadIdx.x == 0) f.key[n] = best;
+        below = best;
+    }
+    if (threadIdx.x == 0) f.count = n;
+    __syncthreads();
+    return n;
+}
+
+// One row by a cluster of C blocks (C = 1: by a block), which take the row's pieces in turn.  A piece is asked for while the one before it
+// is worked on; its maximum and its sums come from registers.  Candidates for the alternatives are values that are not below a bound on the top-th
+// value: the first piece's top-th, raised after every few pieces.  They are few, so a thread that has one reads its values again.
+template <class T, bool TOP>
+__global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C) {
+    constexpr int V = WIDE<T>, NV = ROW_ELEMENTS / V;
+    __shared__ float soft[3][8];
+    __shared__ float mine[3];
     __shared__ Found f;
     const uint32_t tid = threadIdx.x, NT = blockDim.x, rank = blockIdx.x % C;
     const size_t r = blockIdx.x / C;
     const Row<T> row(static_cast<const T *>(a.logits.p) + r * a.logits.stride, (uint32_t)a.vocab);
     const uint32_t pieces = (row.vectors + NT * NV - 1) / (NT * NV);
-    Soft q{-INFINITY, 0.0f, 0.0f};
-    uint32_t held = 0, bound = 0;
-    bool full = false;                       // `held` has top candidates, and the bound is the lowest of them
+    Soft q{-INFINITY, F2(0.0f), F2(0.0f)};
+    uint32_t held = 0, round = 0;
+    float from = -INFINITY;
+    bool lost = false;
     if (TOP && tid == 0) f.count = 0;
-    if (TOP) __syncthreads();
-    for (uint32_t c = rank; c < pieces; c += C) {
+    Pack<T, V> next[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) next[i] = row.load((rank * NV + i) * NT + tid);
+    for (uint32_t c = rank; c < pieces; c += C, round++) {
         Pack<T, V> z[NV];
-        const uint32_t v0 = c * NT * NV + tid;
 #pragma unroll
-        for (int i = 0; i < NV; i++) z[i] = row.load(v0 + i * NT);
-        float m = -INFINITY;
+        for (int i = 0; i < NV; i++) z[i] = next[i];
+        if (c + C < pieces)
 #pragma unroll
-        for (int i = 0; i < NV; i++)
+            for (int i = 0; i < NV; i++) next[i] = row.load(((c + C) * NV + i) * NT + tid);
+        float m = top_of<T>(z[0]);
 #pragma unroll
-            for (int e = 0; e < V; e++) m = fmaxf(m, to_f32(z[i].v[e]));
-        if (m > q.m) q.rise(m);
+        for (int i = 1; i < NV; i++) m = fmaxf(m, top_of<T>(z[i]));
+        if (m != m) m = -INFINITY;
+        q.rise(fmaxf(m, q.m));               // without a branch: behind one the warp's two parts would go through all of the piece by themselves
         const float b = q.base();
 #pragma unroll
         for (int i = 0; i < NV; i++)
 #pragma unroll
-            for (int e = 0; e < V; e++) q.add(to_f32(z[i].v[e]), b);
+            for (int e = 0; e < V; e += 2) q.add(F2(to_f32(z[i].v[e]), to_f32(z[i].v[e + 1])), b);
         if (TOP) {
-            const uint32_t high = order_of(m);
-            if (c == rank) bound = bound_of_top(f, high, a.top);
-            // later pieces have higher indices: with enough candidates a value equal to the bound is too late
-            const uint32_t from = full ? bound + 1 : bound;
-            if (high >= from) {
+            if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
+            // thread by thread, pack by pack, element by element: nearly all end at the first comparison
+            if (m >= from) {
 #pragma unroll
                 for (int i = 0; i < NV; i++)
+                    if (top_of<T>(z[i]) >= from) {
+                        const int64_t first = row.first((c * NV + i) * NT + tid);
 #pragma unroll
-                    for (int e = 0; e < V; e++) {
-                        const float x = to_f32(z[i].v[e]);
-                        const int64_t j = row.first(v0 + i * NT) + e;
-                        if (order_of(x) >= from && j >= 0 && j < (int64_t)row.n) {
-                            const uint32_t at = atomicAdd(&f.count, 1u);
-                            if (at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
+                        for (int e = 0; e < V; e++) {
+                            const float x = to_f32(z[i].v[e]);
+                            const int64_t j = first + e;
+                            if (x >= from && j >= 0 && j < (int64_t)row.n) {
+                                const uint32_t at = atomicAdd(&f.count, 1u);
+                                if (at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
+                            }
                         }
                     }
             }
-            __syncthreads();
-            uint32_t n = f.count;
-            if (n > FOUND) {
-                uint64_t below = ~0ull;
-                n = held;
-                for (uint32_t t = 0; t < a.top; t++) {
-                    uint64_t best = 0;
-#pragma unroll
-                    for (int i = 0; i < NV; i++)
-#pragma unroll
-                        for (int e = 0; e < V; e++) {
-                            const int64_t j = row.first(v0 + i * NT) + e;
-                            if (j < 0 || j >= (int64_t)row.n) continue;
-                            const uint64_t k = key_of(to_f32(z[i].v[e]), (uint32_t)j);
-                            if (k < below && k > best) best = k;
-                        }
-#pragma unroll
-                    for (int o = 16; o; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-                    if ((tid & 31u) == 0) f.most[tid / 32] = best;
-                    __syncthreads();
-                    for (uint32_t w = 0; w < NT / 32; w++) best = max(best, f.most[w]);
-                    __syncthreads();
-                    if (best == 0) break;            // a key of an element is not 0: its index is below 2^32 - 1
-                    if (tid == 0) f.key[n] = best;
-                    n++;
-                    below = best;
-                }
+            __syncwarp();
+            // the bound is raised after 1, 2, 4, ... pieces, in which about as many candidates come as are kept
+            if ((round & (round + 1)) == 0 || c + C >= pieces) {
                 __syncthreads();
-                n = keep_best(f, n, a.top);
-            } else if (!full || n > FOUND / 2) {
-                n = keep_best(f, n, a.top);
+                const uint32_t n = f.count;
+                __syncthreads();
+                lost |= n > FOUND;
+                held = keep_best(f, min(n, FOUND), a.top);
+                // later pieces have higher indices: with enough candidates a value equal to the lowest of them is too late
+                if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.key[a.top - 1] >> 32) + 1));
+                __syncthreads();
             }
-            if (n >= a.top) {
-                if (!full || n == a.top) bound = max(bound, (uint32_t)(f.key[a.top - 1] >> 32));
-                full = true;
-            }
-            held = n;
-            __syncthreads();
-            if (tid == 0) f.count = held;
-            __syncthreads();
         }
     }
+    // too many candidates; or too few, where NaN is among the row's highest
+    if (TOP && (lost || held < a.top)) held = search<T>(f, row, rank, C, pieces, a.top);
     // the threads' sums, then the warps'
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const Soft p{__shfl_xor_sync(0xffffffffu, q.m, o), __shfl_xor_sync(0xffffffffu, q.s, o), __shfl_xor_sync(0xffffffffu, q.w, o)};
-        q.join(p);
+    for (int o = 16; o; o >>= 1) q.join(far(q, o));
+    if ((tid & 31u) == 0) {
+        soft[0][tid / 32] = q.m;
+        soft[1][tid / 32] = q.s.sum();
+        soft[2][tid / 32] = q.w.sum();
     }
-    if ((tid & 31u) == 0) soft[tid / 32] = q;
     __syncthreads();
-    if (tid == 0) {
-        for (uint32_t w = 1; w < NT / 32; w++) q.join(soft[w]);
-        mine = q;
+    if (tid < 32) {
+        // NT / 32 is at most 8: the lanes behind hold nothing
+        const bool some = tid < NT / 32;
+        q = Soft{some ? soft[0][tid] : -INFINITY, F2(some ? soft[1][tid] : 0.0f, 0.0f), F2(some ? soft[2][tid] : 0.0f, 0.0f)};
+#pragma unroll
+        for (int o = 4; o; o >>= 1) q.join(far(q, o));
+        if (tid == 0) {
+            mine[0] = q.m;
+            mine[1] = q.s.sum();
+            mine[2] = q.w.sum();
+        }
     }
-    if (TOP) held = keep_best(f, held, a.top);
-    else __syncthreads();
     if (C > 1) {
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
         if (rank == 0) {
-            if (tid == 0)
-                for (uint32_t o = 1; o < C; o++) q.join(*cluster.map_shared_rank(&mine, o));
+            if (tid < 32) {
+                const bool some = tid < C;
+                const float *there = cluster.map_shared_rank(mine, some ? tid : 0);
+                q = Soft{some ? there[0] : -INFINITY, F2(some ? there[1] : 0.0f, 0.0f), F2(some ? there[2] : 0.0f, 0.0f)};
+#pragma unroll
+                for (int o = 4; o; o >>= 1) q.join(far(q, o));
+            }
             if (TOP) {
-                uint32_t n = held;
-                for (uint32_t o = 1; o < C; o++) {
-                    const Found &far = *cluster.map_shared_rank(&f, o);
-                    const uint32_t more = far.count;
-                    for (uint32_t i = tid; i < more; i += NT) f.key[n + i] = far.key[i];
-                    n += more;
+                for (uint32_t i = tid + a.top; i < C * a.top; i += NT) {
+                    const Found &there = *cluster.map_shared_rank(&f, i / a.top);
+                    f.key[i] = i % a.top < there.count ? there.key[i % a.top] : 0;
                 }
+                for (uint32_t i = tid; i < a.top; i += NT)
+                    if (i >= held) f.key[i] = 0;
                 __syncthreads();
-                keep_best(f, n, a.top);
+                keep_best(f, C * a.top, a.top);
             }
         }
         cluster.sync();                      // nobody leaves while its memory is read
         if (rank) return;
-        if (tid == 0) mine = q;
-        __syncthreads();
+        if (tid == 0) {
+            mine[0] = q.m;
+            mine[1] = q.s.sum();
+            mine[2] = q.w.sum();
+        }
     }
-    q = mine;
-    const bool none = q.s == 0.0f;           // every value is -inf
-    const float ln = logf(q.s), b = q.base();
+    __syncthreads();
+    const float m = mine[0], sum = mine[1];
+    const bool none = sum == 0.0f;           // every value is -inf
+    const float ln = logf(sum), b = m == -INFINITY ? 0.0f : m;
     if (tid == 0) {
         a.lse[r] = none ? -INFINITY : b + ln;
-        a.entropy[r] = none ? 0.0f : ln - q.w / q.s * LN2;
+        a.entropy[r] = none ? 0.0f : ln - mine[2] / sum * LN2;
         const int64_t y = a.targets[r];
         float lp = 0.0f;
         if (y >= (int64_t)row.n) lp = NAN;
