@@ -97,6 +97,40 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return r;
 }
 
+// ---- bulk copies to shared memory, and the barriers that tell of them (by their addresses there) ----
+
+__device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void copies_begin(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+constexpr uint32_t COPY_TRIES = 256;             // of 10 ms at most
+__device__ __forceinline__ bool copies_done(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < COPY_TRIES; i++) {
+        uint32_t done;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+
+// Copies that did not come in time have 20 ms more before their memory is given up.
+static __device__ __noinline__ void copies_lost(int *status) {
+    atomicOr(status, STATUS_COPY);
+    for (int i = 0; i < 20; i++) __nanosleep(1000000);
+}
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barriers_ready() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+// 16-byte aligned both, and a whole number of 16 bytes
+__device__ __forceinline__ void bulk_copy(uint32_t to, uintptr_t from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+
 // Where sample k ends that a row belongs to.  Offsets come from the caller's device memory: whatever they say, `k` stays below
 // `count`, and rows that no sample holds have k == count.
 struct SampleWalk {

@@ -28,7 +28,8 @@ struct LogProbsArgs {
     float *logp, *lse, *entropy, *top_logp;
     int64_t *top_ids;
 };
-cudaError_t launch_log_probs(const LogProbsArgs &a, int dtype, int n_sm, cudaStream_t s);
+// status (here and below): the context's, raised where something inside a kernel does not arrive
+cudaError_t launch_log_probs(const LogProbsArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 struct LogProbsGradArgs {
     MatArg logits;
@@ -51,7 +52,6 @@ struct NormArgs {
     MatOut y;
     float *mean, *rstd;
 };
-// status (of these and of launch_linear_map): the context's, raised where something inside a kernel does not arrive
 cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 // How rows are summed: all of them, or within a sample with the magnitudes added over the samples, or every row a sample of its own.

@@ -39,7 +39,7 @@ int he_token_log_probs(he_ctx *ctx, const void *logits_dev, int dtype, size_t ro
         !natural(top_logp_dev, 4) || !natural(top_ids_dev, 8))
         return HE_ERR_INVALID_ARG;
     const LogProbsArgs a{{logits_dev, row_stride}, rows, vocab, targets_dev, top, logp_dev, lse_dev, entropy_dev, top_logp_dev, top_ids_dev};
-    return done(launch_log_probs(a, dtype, ctx->sm_count, as_stream(stream)));
+    return done(launch_log_probs(a, dtype, ctx->sm_count, ctx->dev.status, as_stream(stream)));
 }
 
 int he_token_log_probs_backward(he_ctx *ctx, const void *logits_dev, int dtype, size_t rows, size_t vocab, size_t row_stride,

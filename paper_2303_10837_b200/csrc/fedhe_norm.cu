@@ -192,7 +192,7 @@ struct Rows {
         const uint32_t n = size(row);
         if (!EVEN && !n) return;
         const uint32_t to = EVEN ? room : room + (uint32_t)(from(row) - (row & ~(uintptr_t)15));
-        asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from(row)), "r"(n), "r"(bar) : "memory");
+        bulk_copy(to, from(row), n, bar);
     }
     // A thread's packs of a row that has been copied; zeros behind its end.  A matrix's first and last bytes that no copy brings come from where they are.
     template <int V, int K>
@@ -215,29 +215,6 @@ struct Rows {
         }
     }
 };
-
-__device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copies_begin(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-constexpr uint32_t COPY_TRIES = 256;             // of 10 ms at most
-__device__ __forceinline__ bool copies_done(uint32_t bar, uint32_t parity) {
-    for (uint32_t i = 0; i < COPY_TRIES; i++) {
-        uint32_t done;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 0x989680;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(done)
-                     : "r"(bar), "r"(parity)
-                     : "memory");
-        if (done) return true;
-    }
-    return false;
-}
-
-// Copies that did not come in time have 20 ms more before their memory is given up.
-__device__ __noinline__ void copies_lost(int *status) {
-    atomicOr(status, STATUS_COPY);
-    for (int i = 0; i < 20; i++) __nanosleep(1000000);
-}
 
 // The sum over the first `lanes` lanes (a power of two; the others hold the same again); the same bits in every lane.
 __device__ __forceinline__ float few_sum(float v, uint32_t lanes) {
@@ -314,8 +291,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
         asked_at += stride;
     };
     if (t == 0) {
-        for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + d * 8) : "memory");
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (uint32_t d = 0; d < plan.depth; d++) barrier_init(bar + d * 8, 1);
+        barriers_ready();
         for (uint32_t d = 0; d < plan.depth; d++) ask(d);
     }
     F2 w[HELD / 2], b[HELD / 2];
@@ -430,8 +407,8 @@ __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGr
             dy_asked += dys.pitch;
         };
         if (t == 0) {
-            for (uint32_t d = 0; d < plan.depth; d++) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + d * 8) : "memory");
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            for (uint32_t d = 0; d < plan.depth; d++) barrier_init(bar + d * 8, 1);
+            barriers_ready();
             for (uint32_t d = 0; d < plan.depth; d++) ask(d);
         }
         F2 w[HELD / 2];

@@ -16,8 +16,10 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float FAR = -1e30f;             // exponents stop here: 2^FAR is 0, and FAR times 0 is 0, not NaN
-constexpr int ROW_ELEMENTS = 32;          // of a thread, at a time
-constexpr uint32_t FOUND = 1024;          // candidates that a block can hold
+constexpr int PACKS = 4;                  // of 16 bytes, that a thread has of a piece
+constexpr uint32_t FOUND = 512;           // candidates that a block can hold
+constexpr uint32_t DEPTH = 4;             // pieces that a warp asks for ahead
+constexpr uint32_t PIECE_BYTES = 32 * PACKS * 16;      // of a warp
 
 __device__ __forceinline__ float ex2(float x) {
     float r;
@@ -162,10 +164,10 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
 }
 
 // The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are as high as the
-// bound that the candidates have no room.
+// bound that the candidates have no room, or NaN is among the highest.
 template <class T>
 __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t first, uint32_t step, uint32_t pieces, uint32_t top) {
-    constexpr int V = WIDE<T>, NV = ROW_ELEMENTS / V;
+    constexpr int V = WIDE<T>;
     const uint32_t NT = blockDim.x;
     uint64_t below = ~0ull;
     uint32_t n = 0;
@@ -173,8 +175,8 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
     for (; n < top; n++) {
         uint64_t best = 0;
         for (uint32_t c = first; c < pieces; c += step)
-            for (uint32_t i = 0; i < NV; i++) {
-                const uint32_t v = (c * NV + i) * NT + threadIdx.x;
+            for (uint32_t i = 0; i < PACKS; i++) {
+                const uint32_t v = (c * PACKS + i) * NT + threadIdx.x;
                 if (v >= row.vectors) break;
                 const Pack<T, V> p = row.load(v);
 #pragma unroll
@@ -199,174 +201,238 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
     return n;
 }
 
-// One row by a cluster of C blocks (C = 1: by a block), which take the row's pieces in turn.  A piece is asked for while the one before it
-// is worked on; its maximum and its sums come from registers.  Candidates for the alternatives are values that are not below a bound on the top-th
-// value: the first piece's top-th, raised after every few pieces.  They are few, so a thread that has one reads its values again.
+// Rows by clusters of C blocks (C = 1: by blocks), which take a row's pieces in turn; each warp has its part of a piece, PIECE_BYTES in a row, and
+// asks for its parts by bulk copies, DEPTH ahead and on into the next row (asked for in registers, one ahead: 307 us for 2048 x
+// 131072 in bf16 with eight alternatives; so ...).  Candidates for the alternatives are values that are not below a bound on the top-th value: that
+// of the pieces so far, raised after 1, 2, 4, ... of them.
 template <class T, bool TOP>
-__global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C) {
-    constexpr int V = WIDE<T>, NV = ROW_ELEMENTS / V;
+__global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C, int *status) {
+    constexpr int V = WIDE<T>;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ uint64_t bars[8][DEPTH];
     __shared__ float soft[3][8];
     __shared__ float mine[3];
     __shared__ Found f;
-    const uint32_t tid = threadIdx.x, NT = blockDim.x, rank = blockIdx.x % C;
-    const size_t r = blockIdx.x / C;
-    const Row<T> row(static_cast<const T *>(a.logits.p) + r * a.logits.stride, (uint32_t)a.vocab);
-    const uint32_t pieces = (row.vectors + NT * NV - 1) / (NT * NV);
-    Soft q{-INFINITY, F2(0.0f), F2(0.0f)};
-    uint32_t held = 0, round = 0;
-    float from = -INFINITY;
-    bool lost = false;
-    if (TOP && tid == 0) f.count = 0;
-    Pack<T, V> next[NV];
-#pragma unroll
-    for (int i = 0; i < NV; i++) next[i] = row.load((rank * NV + i) * NT + tid);
-    for (uint32_t c = rank; c < pieces; c += C, round++) {
-        Pack<T, V> z[NV];
-#pragma unroll
-        for (int i = 0; i < NV; i++) z[i] = next[i];
-        if (c + C < pieces)
-#pragma unroll
-            for (int i = 0; i < NV; i++) next[i] = row.load(((c + C) * NV + i) * NT + tid);
-        float m = top_of<T>(z[0]);
-#pragma unroll
-        for (int i = 1; i < NV; i++) m = fmaxf(m, top_of<T>(z[i]));
-        if (m != m) m = -INFINITY;
-        q.rise(fmaxf(m, q.m));               // without a branch: behind one the warp's two parts would go through all of the piece by themselves
-        const float b = q.base();
-#pragma unroll
-        for (int i = 0; i < NV; i++)
-#pragma unroll
-            for (int e = 0; e < V; e += 2) q.add(F2(to_f32(z[i].v[e]), to_f32(z[i].v[e + 1])), b);
+    const uint32_t tid = threadIdx.x, NT = blockDim.x, warp = tid / 32, lane = tid & 31u, rank = blockIdx.x % C, clusters = gridDim.x / C;
+    const uint32_t rows = (uint32_t)a.rows, first_row = blockIdx.x / C, n = (uint32_t)a.vocab;
+    const size_t pitch = a.logits.stride * sizeof(T);
+    const uintptr_t base = reinterpret_cast<uintptr_t>(a.logits.p);
+    // whole 16 bytes of the matrix: no copy reaches outside
+    const uintptr_t low = (base + 15) & ~(uintptr_t)15, high = (base + (rows - 1) * pitch + (size_t)n * sizeof(T)) & ~(uintptr_t)15;
+    uint8_t *room = ring + warp * DEPTH * PIECE_BYTES;
+    const uint32_t room_at = shared_at(room), bar = shared_at(&bars[warp][0]);
+    // by a warp's first lane: the piece to ask for next
+    uint32_t asked_row = first_row, asked = rank;
+    const auto ask = [&](uint32_t d) {
+        if (asked_row >= rows) return;
+        const uintptr_t row = base + asked_row * pitch, start = row & ~(uintptr_t)15;
+        uintptr_t from = start + (size_t)(asked * NT + warp * 32) * (PACKS * 16), to = from + PIECE_BYTES;
+        uintptr_t end = (row + (size_t)n * sizeof(T) + 15) & ~(uintptr_t)15;
+        const uint32_t pieces = (uint32_t)((end - start + NT * (PACKS * 16) - 1) / (NT * (PACKS * 16)));
+        end = end < high ? end : high;
+        const uintptr_t at = from < low ? low : from;
+        to = to < end ? to : end;
+        const uint32_t bytes = to > at ? (uint32_t)(to - at) : 0;
+        copies_begin(bar + d * 8, bytes);
+        if (bytes) bulk_copy(room_at + d * PIECE_BYTES + (uint32_t)(at - from), at, bytes, bar + d * 8);
+        asked += C;
+        if (asked >= pieces) asked = rank, asked_row += clusters;
+    };
+    if (lane == 0) {
+        for (uint32_t d = 0; d < DEPTH; d++) barrier_init(bar + d * 8, 1);
+        barriers_ready();
+        for (uint32_t d = 0; d < DEPTH; d++) ask(d);
+    }
+    __syncwarp();
+    uint32_t d = 0, turn = 0;
+    bool gone = false;                       // a copy did not come: none is waited for any more
+    for (uint32_t r = first_row; r < rows; r += clusters) {
+        const Row<T> row(reinterpret_cast<const T *>(base + r * pitch), n);
+        const uint32_t pieces = (row.vectors + NT * PACKS - 1) / (NT * PACKS);
+        Soft q{-INFINITY, F2(0.0f), F2(0.0f)};
+        uint32_t held = 0, round = 0;
+        float from = -INFINITY;
+        bool lost = false;
         if (TOP) {
-            if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
-            // thread by thread, pack by pack, element by element: nearly all end at the first comparison
-            if (m >= from) {
+            if (tid == 0) f.count = 0;
+            __syncthreads();
+        }
+        for (uint32_t c = rank; c < pieces; c += C, round++) {
+            if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
+            Pack<T, V> z[PACKS];
+            const uint32_t v0 = (c * NT + warp * 32) * PACKS + lane;
 #pragma unroll
-                for (int i = 0; i < NV; i++)
-                    if (top_of<T>(z[i]) >= from) {
-                        const int64_t first = row.first((c * NV + i) * NT + tid);
+            for (int i = 0; i < PACKS; i++) {
+                const uint32_t v = v0 + i * 32;
+                const uint8_t *in = room + d * PIECE_BYTES + (i * 32 + lane) * 16;
+                if (v >= row.vectors) {
 #pragma unroll
-                        for (int e = 0; e < V; e++) {
-                            const float x = to_f32(z[i].v[e]);
-                            const int64_t j = first + e;
-                            if (x >= from && j >= 0 && j < (int64_t)row.n) {
-                                const uint32_t at = atomicAdd(&f.count, 1u);
-                                if (at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
-                            }
-                        }
-                    }
+                    for (int e = 0; e < V; e++) z[i].v[e] = from_f32<T>(-INFINITY);
+                } else if (row.whole(v)) {
+                    z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in));
+                } else {
+                    z[i] = row.load(v);
+                }
             }
             __syncwarp();
-            // the bound is raised after 1, 2, 4, ... pieces, in which about as many candidates come as are kept
-            if ((round & (round + 1)) == 0 || c + C >= pieces) {
-                __syncthreads();
-                const uint32_t n = f.count;
-                __syncthreads();
-                lost |= n > FOUND;
-                held = keep_best(f, min(n, FOUND), a.top);
-                // later pieces have higher indices: with enough candidates a value equal to the lowest of them is too late
-                if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.key[a.top - 1] >> 32) + 1));
-                __syncthreads();
-            }
-        }
-    }
-    // too many candidates; or too few, where NaN is among the row's highest
-    if (TOP && (lost || held < a.top)) held = search<T>(f, row, rank, C, pieces, a.top);
-    // the threads' sums, then the warps'
+            if (lane == 0) ask(d);
+            if (++d == DEPTH) d = 0, turn ^= 1u;
+            float m = top_of<T>(z[0]);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) q.join(far(q, o));
-    if ((tid & 31u) == 0) {
-        soft[0][tid / 32] = q.m;
-        soft[1][tid / 32] = q.s.sum();
-        soft[2][tid / 32] = q.w.sum();
-    }
-    __syncthreads();
-    if (tid < 32) {
-        // NT / 32 is at most 8: the lanes behind hold nothing
-        const bool some = tid < NT / 32;
-        q = Soft{some ? soft[0][tid] : -INFINITY, F2(some ? soft[1][tid] : 0.0f, 0.0f), F2(some ? soft[2][tid] : 0.0f, 0.0f)};
+            for (int i = 1; i < PACKS; i++) m = fmaxf(m, top_of<T>(z[i]));
+            if (m != m) m = -INFINITY;
+            q.rise(fmaxf(m, q.m));           // without a branch: behind one the warp's two parts would go through all of the piece by themselves
+            const float b = q.base();
 #pragma unroll
-        for (int o = 4; o; o >>= 1) q.join(far(q, o));
-        if (tid == 0) {
-            mine[0] = q.m;
-            mine[1] = q.s.sum();
-            mine[2] = q.w.sum();
-        }
-    }
-    if (C > 1) {
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();
-        if (rank == 0) {
-            if (tid < 32) {
-                const bool some = tid < C;
-                const float *there = cluster.map_shared_rank(mine, some ? tid : 0);
-                q = Soft{some ? there[0] : -INFINITY, F2(some ? there[1] : 0.0f, 0.0f), F2(some ? there[2] : 0.0f, 0.0f)};
+            for (int i = 0; i < PACKS; i++)
 #pragma unroll
-                for (int o = 4; o; o >>= 1) q.join(far(q, o));
-            }
+                for (int e = 0; e < V; e += 2) q.add(F2(to_f32(z[i].v[e]), to_f32(z[i].v[e + 1])), b);
             if (TOP) {
-                for (uint32_t i = tid + a.top; i < C * a.top; i += NT) {
-                    const Found &there = *cluster.map_shared_rank(&f, i / a.top);
-                    f.key[i] = i % a.top < there.count ? there.key[i % a.top] : 0;
+                if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
+                // thread by thread, pack by pack, element by element: nearly all end at the first comparison
+                if (m >= from) {
+#pragma unroll
+                    for (int i = 0; i < PACKS; i++)
+                        if (top_of<T>(z[i]) >= from) {
+                            const int64_t first = row.first(v0 + i * 32);
+#pragma unroll
+                            for (int e = 0; e < V; e++) {
+                                const float x = to_f32(z[i].v[e]);
+                                const int64_t j = first + e;
+                                if (x >= from && j >= 0 && j < (int64_t)row.n) {
+                                    const uint32_t at = atomicAdd(&f.count, 1u);
+                                    if (at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
+                                }
+                            }
+                        }
                 }
-                for (uint32_t i = tid; i < a.top; i += NT)
-                    if (i >= held) f.key[i] = 0;
-                __syncthreads();
-                keep_best(f, C * a.top, a.top);
+                __syncwarp();
+                // the bound is raised after 1, 2, 4, ... pieces, in which about as many candidates come as are kept
+                if ((round & (round + 1)) == 0 || c + C >= pieces) {
+                    __syncthreads();
+                    const uint32_t found = f.count;
+                    __syncthreads();
+                    lost |= found > FOUND;
+                    held = keep_best(f, min(found, FOUND), a.top);
+                    // later pieces have higher indices: with enough candidates a value equal to the lowest of them is too late
+                    if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.key[a.top - 1] >> 32) + 1));
+                    __syncthreads();
+                }
             }
         }
-        cluster.sync();                      // nobody leaves while its memory is read
-        if (rank) return;
+        // too many candidates; or too few, where NaN is among the row's highest
+        if (TOP && (lost || held < a.top)) held = search<T>(f, row, rank, C, pieces, a.top);
+        // the threads' sums, then the warps'
+#pragma unroll
+        for (int o = 16; o; o >>= 1) q.join(far(q, o));
+        if (lane == 0) {
+            soft[0][warp] = q.m;
+            soft[1][warp] = q.s.sum();
+            soft[2][warp] = q.w.sum();
+        }
+        __syncthreads();
+        if (tid < 32) {
+            // NT / 32 is at most 8: the lanes behind hold nothing
+            const bool some = tid < NT / 32;
+            q = Soft{some ? soft[0][tid] : -INFINITY, F2(some ? soft[1][tid] : 0.0f, 0.0f), F2(some ? soft[2][tid] : 0.0f, 0.0f)};
+#pragma unroll
+            for (int o = 4; o; o >>= 1) q.join(far(q, o));
+            if (tid == 0) {
+                mine[0] = q.m;
+                mine[1] = q.s.sum();
+                mine[2] = q.w.sum();
+            }
+        }
+        if (C > 1) {
+            cg::cluster_group cluster = cg::this_cluster();
+            cluster.sync();
+            if (rank == 0) {
+                if (tid < 32) {
+                    const bool some = tid < C;
+                    const float *there = cluster.map_shared_rank(mine, some ? tid : 0);
+                    q = Soft{some ? there[0] : -INFINITY, F2(some ? there[1] : 0.0f, 0.0f), F2(some ? there[2] : 0.0f, 0.0f)};
+#pragma unroll
+                    for (int o = 4; o; o >>= 1) q.join(far(q, o));
+                }
+                if (TOP) {
+                    for (uint32_t i = tid + a.top; i < C * a.top; i += NT) {
+                        const Found &there = *cluster.map_shared_rank(&f, i / a.top);
+                        f.key[i] = i % a.top < there.count ? there.key[i % a.top] : 0;
+                    }
+                    for (uint32_t i = tid; i < a.top; i += NT)
+                        if (i >= held) f.key[i] = 0;
+                    __syncthreads();
+                    keep_best(f, C * a.top, a.top);
+                }
+            }
+            cluster.sync();                  // nobody goes on while its memory is read
+            if (rank) continue;
+            if (tid == 0) {
+                mine[0] = q.m;
+                mine[1] = q.s.sum();
+                mine[2] = q.w.sum();
+            }
+        }
+        __syncthreads();
+        const float m = mine[0], sum = mine[1];
+        const bool none = sum == 0.0f;       // every value is -inf
+        const float ln = logf(sum), b = m == -INFINITY ? 0.0f : m;
         if (tid == 0) {
-            mine[0] = q.m;
-            mine[1] = q.s.sum();
-            mine[2] = q.w.sum();
+            a.lse[r] = none ? -INFINITY : b + ln;
+            a.entropy[r] = none ? 0.0f : ln - mine[2] / sum * LN2;
+            const int64_t y = a.targets[r];
+            float lp = 0.0f;
+            if (y >= (int64_t)row.n) lp = NAN;
+            else if (y >= 0) lp = none ? -INFINITY : (to_f32(row.p[y]) - b) - ln;
+            a.logp[r] = lp;
         }
-    }
-    __syncthreads();
-    const float m = mine[0], sum = mine[1];
-    const bool none = sum == 0.0f;           // every value is -inf
-    const float ln = logf(sum), b = m == -INFINITY ? 0.0f : m;
-    if (tid == 0) {
-        a.lse[r] = none ? -INFINITY : b + ln;
-        a.entropy[r] = none ? 0.0f : ln - mine[2] / sum * LN2;
-        const int64_t y = a.targets[r];
-        float lp = 0.0f;
-        if (y >= (int64_t)row.n) lp = NAN;
-        else if (y >= 0) lp = none ? -INFINITY : (to_f32(row.p[y]) - b) - ln;
-        a.logp[r] = lp;
-    }
-    if (TOP)
-        for (uint32_t i = tid; i < a.top; i += NT) {
-            const uint64_t k = f.key[i];
-            a.top_ids[r * a.top + i] = (int64_t)(0xffffffffu - (uint32_t)k);
-            a.top_logp[r * a.top + i] = none ? -INFINITY : (value_of((uint32_t)(k >> 32)) - b) - ln;
+        if (TOP) {
+            for (uint32_t i = tid; i < a.top; i += NT) {
+                const uint64_t k = f.key[i];
+                a.top_ids[(size_t)r * a.top + i] = (int64_t)(0xffffffffu - (uint32_t)k);
+                a.top_logp[(size_t)r * a.top + i] = none ? -INFINITY : (value_of((uint32_t)(k >> 32)) - b) - ln;
+            }
         }
+        __syncthreads();                     // `mine` and the candidates are the next row's
+    }
+    if (gone) copies_lost(status);
 }
 
-// Threads of a block: as few as hold a row of up to 256 * 32 elements at once.
-inline uint32_t row_threads(size_t vocab) {
-    const size_t t = (vocab + ROW_ELEMENTS - 1) / ROW_ELEMENTS;
+// Threads of a block: as few as hold a row of up to 256 threads' packs at once.
+inline uint32_t row_threads(size_t bytes) {
+    const size_t t = (bytes + 15 + PACKS * 16 - 1) / (PACKS * 16);
     return t >= 256 ? 256 : (uint32_t)(t + 31) / 32 * 32;
 }
 
 template <class T>
-cudaError_t log_probs_of(const LogProbsArgs &a, int n_sm, cudaStream_t s) {
-    const uint32_t nt = row_threads(a.vocab);
-    const size_t pieces = (a.vocab + WIDE<T> + (size_t)nt * ROW_ELEMENTS - 1) / ((size_t)nt * ROW_ELEMENTS);
+cudaError_t log_probs_of(const LogProbsArgs &a, int n_sm, int *status, cudaStream_t s) {
+    const uint32_t nt = row_threads(a.vocab * sizeof(T));
+    const size_t pieces = (a.vocab * sizeof(T) + 15 + (size_t)nt * PACKS * 16 - 1) / ((size_t)nt * PACKS * 16);
+    const uint32_t bytes = nt / 32 * DEPTH * PIECE_BYTES;
+    // blocks that an SM holds: 768 threads by the registers, and shared memory
+    uint32_t held = 768 / nt;
+    const uint32_t by_memory = (uint32_t)((222u << 10) / (bytes + (a.top ? sizeof(Found) : 0) + 1536));
+    if (held > by_memory) held = by_memory;
+    if (held > 24) held = 24;
+    const size_t most = (size_t)held * n_sm;
     // few rows: a cluster of up to eight blocks shares one, as long as each has a piece
     uint32_t C = 1;
-    while (C < 8 && 2 * C <= pieces && a.rows * 2 * C <= (size_t)4 * n_sm) C *= 2;
+    while (C < 8 && 2 * C <= pieces && a.rows * 2 * C <= most + n_sm) C *= 2;
+    const size_t clusters = most / C ? most / C : 1;
+    const auto kernel = a.top ? log_probs_kernel<T, true> : log_probs_kernel<T, false>;
+    cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (rc != cudaSuccess) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(nt);
+    cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim = {C, 1, 1};
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    cfg.gridDim = dim3((unsigned)(a.rows * C));
-    const cudaError_t rc = a.top ? cudaLaunchKernelEx(&cfg, log_probs_kernel<T, true>, a, C) : cudaLaunchKernelEx(&cfg, log_probs_kernel<T, false>, a, C);
+    cfg.gridDim = dim3((unsigned)((C > 1 || a.rows < clusters ? a.rows : clusters) * C));
+    rc = cudaLaunchKernelEx(&cfg, kernel, a, C, status);
     if (rc != cudaSuccess) return rc;
     return FEDHE_LAUNCHED();
 }
@@ -448,10 +514,10 @@ cudaError_t log_probs_grad_of(const LogProbsGradArgs &a, int n_sm, cudaStream_t 
 
 }  // namespace
 
-cudaError_t launch_log_probs(const LogProbsArgs &a, int dtype, int n_sm, cudaStream_t s) {
-    return dtype == HE_F32    ? log_probs_of<float>(a, n_sm, s)
-           : dtype == HE_BF16 ? log_probs_of<__nv_bfloat16>(a, n_sm, s)
-                              : log_probs_of<__half>(a, n_sm, s);
+cudaError_t launch_log_probs(const LogProbsArgs &a, int dtype, int n_sm, int *status, cudaStream_t s) {
+    return dtype == HE_F32    ? log_probs_of<float>(a, n_sm, status, s)
+           : dtype == HE_BF16 ? log_probs_of<__nv_bfloat16>(a, n_sm, status, s)
+                              : log_probs_of<__half>(a, n_sm, status, s);
 }
 
 cudaError_t launch_log_probs_grad(const LogProbsGradArgs &a, int dtype, int n_sm, cudaStream_t s) {
