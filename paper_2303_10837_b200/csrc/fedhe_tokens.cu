@@ -41,9 +41,10 @@ struct Soft {
     }
     __device__ __forceinline__ void add(F2 z, float b) {
         const float2 t = ((z + F2(-b)) * F2(LOG2E)).both();
-        const F2 u(max_nan(t.x, FAR), max_nan(t.y, FAR)), e(ex2(max_nan(t.x, FAR)), ex2(max_nan(t.y, FAR)));
+        const float x = max_nan(t.x, FAR), y = max_nan(t.y, FAR);
+        const F2 e(ex2(x), ex2(y));
         s = s + e;
-        w = fma2(e, u, w);
+        w = fma2(e, F2(x, y), w);
     }
     __device__ __forceinline__ void join(Soft o) {
         const float to = fmaxf(m, o.m);
@@ -221,26 +222,33 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
     const uintptr_t low = (base + 15) & ~(uintptr_t)15, high = (base + (rows - 1) * pitch + (size_t)n * sizeof(T)) & ~(uintptr_t)15;
     uint8_t *room = ring + warp * DEPTH * PIECE_BYTES;
     const uint32_t room_at = shared_at(room), bar = shared_at(&bars[warp][0]);
-    // by a warp's first lane: the piece to ask for next
-    uint32_t asked_row = first_row, asked = rank;
+    // by a warp's first lane: the piece to ask for next, where it and its row's end are, and the row's pieces
+    uint32_t asked_row = first_row, asked = rank, asked_pieces = 0;
+    uintptr_t asked_at = 0, asked_end = 0;
+    const auto enter = [&] {
+        const uintptr_t row = base + asked_row * pitch, start = row & ~(uintptr_t)15, end = (row + (size_t)n * sizeof(T) + 15) & ~(uintptr_t)15;
+        asked_pieces = ((uint32_t)((end - start) / 16) + NT * PACKS - 1) / (NT * PACKS);
+        asked_at = start + (size_t)(rank * NT + warp * 32) * (PACKS * 16);
+        asked_end = end < high ? end : high;
+        asked = rank;
+    };
     const auto ask = [&](uint32_t d) {
         if (asked_row >= rows) return;
-        const uintptr_t row = base + asked_row * pitch, start = row & ~(uintptr_t)15;
-        uintptr_t from = start + (size_t)(asked * NT + warp * 32) * (PACKS * 16), to = from + PIECE_BYTES;
-        uintptr_t end = (row + (size_t)n * sizeof(T) + 15) & ~(uintptr_t)15;
-        const uint32_t pieces = (uint32_t)((end - start + NT * (PACKS * 16) - 1) / (NT * (PACKS * 16)));
-        end = end < high ? end : high;
-        const uintptr_t at = from < low ? low : from;
-        to = to < end ? to : end;
+        const uintptr_t at = asked_at < low ? low : asked_at, to = asked_at + PIECE_BYTES < asked_end ? asked_at + PIECE_BYTES : asked_end;
         const uint32_t bytes = to > at ? (uint32_t)(to - at) : 0;
         copies_begin(bar + d * 8, bytes);
-        if (bytes) bulk_copy(room_at + d * PIECE_BYTES + (uint32_t)(at - from), at, bytes, bar + d * 8);
+        if (bytes) bulk_copy(room_at + d * PIECE_BYTES + (uint32_t)(at - asked_at), at, bytes, bar + d * 8);
         asked += C;
-        if (asked >= pieces) asked = rank, asked_row += clusters;
+        asked_at += (size_t)C * NT * (PACKS * 16);
+        if (asked >= asked_pieces) {
+            asked_row += clusters;
+            enter();
+        }
     };
     if (lane == 0) {
         for (uint32_t d = 0; d < DEPTH; d++) barrier_init(bar + d * 8, 1);
         barriers_ready();
+        enter();
         for (uint32_t d = 0; d < DEPTH; d++) ask(d);
     }
     __syncwarp();
