@@ -46,18 +46,16 @@ struct Soft {
         s = s + e;
         w = fma2(e, F2(x, y), w);
     }
-    __device__ __forceinline__ void join(Soft o) {
-        const float to = fmaxf(m, o.m);
+    // the lanes' to one, in every lane
+    __device__ __forceinline__ void join_warp() {
+        float to = m;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
         rise(to);
-        o.rise(to);
-        s = s + o.s;
-        w = w + o.w;
+        s = F2(warp_sum(s.sum()), 0.0f);
+        w = F2(warp_sum(w.sum()), 0.0f);
     }
 };
-__device__ __forceinline__ Soft far(const Soft &q, int o) {       // another lane's, its two sums as one
-    const float s = q.s.sum(), w = q.w.sum();
-    return Soft{__shfl_xor_sync(0xffffffffu, q.m, o), F2(__shfl_xor_sync(0xffffffffu, s, o), 0.0f), F2(__shfl_xor_sync(0xffffffffu, w, o), 0.0f)};
-}
 
 // Order of the alternatives: the value, NaN as low as -inf, then the lowest index.
 __device__ __forceinline__ uint32_t order_of(float z) {
@@ -126,7 +124,7 @@ __device__ __forceinline__ float top_of<__half>(const Pack<__half, 8> &p) {
 struct Found {
     uint64_t key[FOUND];
     uint64_t best[HE_MAX_TOP];
-    uint32_t count, bound[8];
+    uint32_t count, bound[8], from;          // from: order of what a candidate has at least
     uint64_t most[8];
 };
 
@@ -162,6 +160,21 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
     uint32_t low = f.bound[0];
     for (uint32_t i = 1; i < warps; i++) low = min(low, f.bound[i]);
     return low;
+}
+
+// Raises the bound to the top-th of the candidates that are there; by a warp, while others add to them (a place that is not written yet is 0).
+__device__ __forceinline__ void raise_bound(Found &f, uint32_t top) {
+    __syncwarp();
+    const uint32_t n = min(*(volatile uint32_t *)&f.count, FOUND);
+    if (n < top) return;
+    for (uint32_t i = threadIdx.x & 31u; i < n; i += 32) {
+        const uint64_t mine = *(volatile uint64_t *)&f.key[i];
+        uint32_t above = 0;
+#pragma unroll 8
+        for (uint32_t j = 0; j < n; j++) above += f.key[j] > mine;
+        if (mine && above == top - 1) atomicMax(&f.from, (uint32_t)(mine >> 32));
+    }
+    __syncwarp();
 }
 
 // The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are as high as the
@@ -204,8 +217,9 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
 
 // Rows by clusters of C blocks (C = 1: by blocks), which take a row's pieces in turn; each warp has its part of a piece, PIECE_BYTES in a row, and
 // asks for its parts by bulk copies, DEPTH ahead and on into the next row (asked for in registers, one ahead: 307 us for 2048 x
-// 131072 in bf16 with eight alternatives; so ...).  Candidates for the alternatives are values that are not below a bound on the top-th value: that
-// of the pieces so far, raised after 1, 2, 4, ... of them.
+// 131072 in bf16 with eight alternatives; so 193).  Candidates for the alternatives are values that are not below a bound on the top-th value,
+// which the warps raise in turn after 1, 2, 4, ... pieces, in which about as many candidates come as are wanted; they do not wait for one another
+// (with the candidates cut down by the whole block each time: 180 us, without alternatives 127).
 template <class T, bool TOP>
 __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C, int *status) {
     constexpr int V = WIDE<T>;
@@ -259,32 +273,36 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         const uint32_t pieces = (row.vectors + NT * PACKS - 1) / (NT * PACKS);
         Soft q{-INFINITY, F2(0.0f), F2(0.0f)};
         uint32_t held = 0, round = 0;
-        float from = -INFINITY;
-        bool lost = false;
+        // vectors that lie in the row as a whole
+        const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V;
         if (TOP) {
-            if (tid == 0) f.count = 0;
+            for (uint32_t i = tid; i < FOUND; i += NT) f.key[i] = 0;
+            if (tid == 0) f.count = f.from = 0;
             __syncthreads();
         }
         for (uint32_t c = rank; c < pieces; c += C, round++) {
             if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
             Pack<T, V> z[PACKS];
             const uint32_t v0 = (c * NT + warp * 32) * PACKS + lane;
+            const uint8_t *in = room + d * PIECE_BYTES + lane * 16;
+            const bool inside = v0 - lane >= whole_from && v0 - lane + 32 * PACKS <= whole_to;
+            if (inside) {
 #pragma unroll
-            for (int i = 0; i < PACKS; i++) {
-                const uint32_t v = v0 + i * 32;
-                const uint8_t *in = room + d * PIECE_BYTES + (i * 32 + lane) * 16;
-                if (v >= row.vectors) {
+                for (int i = 0; i < PACKS; i++) z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in + i * 512));
+            } else {
 #pragma unroll
-                    for (int e = 0; e < V; e++) z[i].v[e] = from_f32<T>(-INFINITY);
-                } else if (row.whole(v)) {
-                    z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in));
-                } else {
-                    z[i] = row.load(v);
+                for (int i = 0; i < PACKS; i++) {
+                    const uint32_t v = v0 + i * 32;
+                    if (v >= row.vectors) {
+#pragma unroll
+                        for (int e = 0; e < V; e++) z[i].v[e] = from_f32<T>(-INFINITY);
+                    } else if (v >= whole_from && v < whole_to) {
+                        z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in + i * 512));
+                    } else {
+                        z[i] = row.load(v);
+                    }
                 }
             }
-            __syncwarp();
-            if (lane == 0) ask(d);
-            if (++d == DEPTH) d = 0, turn ^= 1u;
             float m = top_of<T>(z[0]);
 #pragma unroll
             for (int i = 1; i < PACKS; i++) m = fmaxf(m, top_of<T>(z[i]));
@@ -296,43 +314,41 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
 #pragma unroll
                 for (int e = 0; e < V; e += 2) q.add(F2(to_f32(z[i].v[e]), to_f32(z[i].v[e + 1])), b);
             if (TOP) {
-                if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
-                // thread by thread, pack by pack, element by element: nearly all end at the first comparison
-                if (m >= from) {
-#pragma unroll
-                    for (int i = 0; i < PACKS; i++)
-                        if (top_of<T>(z[i]) >= from) {
-                            const int64_t first = row.first(v0 + i * 32);
-#pragma unroll
-                            for (int e = 0; e < V; e++) {
-                                const float x = to_f32(z[i].v[e]);
-                                const int64_t j = first + e;
-                                if (x >= from && j >= 0 && j < (int64_t)row.n) {
-                                    const uint32_t at = atomicAdd(&f.count, 1u);
-                                    if (at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
-                                }
-                            }
-                        }
+                if (round == 0) {
+                    const uint32_t bound = bound_of_top(f, order_of(m), a.top);
+                    if (lane == 0) atomicMax(&f.from, bound);
+                    __syncwarp();
+                } else if ((round & (round - 1)) == 0 && __clz((int)round) % (NT / 32) == warp) {
+                    raise_bound(f, a.top);
                 }
-                __syncwarp();
-                // the bound is raised after 1, 2, 4, ... pieces, in which about as many candidates come as are kept
-                if ((round & (round + 1)) == 0 || c + C >= pieces) {
-                    __syncthreads();
-                    const uint32_t found = f.count;
-                    __syncthreads();
-                    lost |= found > FOUND;
-                    held = keep_best(f, min(found, FOUND), a.top);
-                    // later pieces have higher indices: with enough candidates a value equal to the lowest of them is too late
-                    if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.key[a.top - 1] >> 32) + 1));
-                    __syncthreads();
+                const float from = value_of(*(volatile uint32_t *)&f.from);
+                // threads that have a candidate, few: the warp looks through the values of one after the other, a lane at each value
+                for (uint32_t who = __ballot_sync(0xffffffffu, m >= from); who; who &= who - 1) {
+                    const uint32_t l = __ffs(who) - 1, i = lane / V, e = lane % V;
+                    const int64_t j = row.first(v0 - lane + i * 32 + l) + e;
+                    bool hit = i < PACKS && j >= 0 && j < (int64_t)row.n;
+                    const float x = !hit ? 0.0f : to_f32(inside ? reinterpret_cast<const T *>(in - lane * 16 + (i * 32 + l) * 16)[e] : row.p[j]);
+                    hit = hit && x >= from;
+                    const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+                    uint32_t at = 0;
+                    if (lane == 0) at = atomicAdd(&f.count, __popc(hits));
+                    at = __shfl_sync(0xffffffffu, at, 0) + __popc(hits & ((1u << lane) - 1));
+                    if (hit && at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
+                    __syncwarp();
                 }
             }
+            __syncwarp();
+            if (lane == 0) ask(d);
+            if (++d == DEPTH) d = 0, turn ^= 1u;
         }
-        // too many candidates; or too few, where NaN is among the row's highest
-        if (TOP && (lost || held < a.top)) held = search<T>(f, row, rank, C, pieces, a.top);
+        if (TOP) {
+            __syncthreads();
+            const uint32_t found = f.count;
+            // too many candidates; or too few, where NaN is among the row's highest
+            held = found < a.top || found > FOUND ? search<T>(f, row, rank, C, pieces, a.top) : keep_best(f, found, a.top);
+        }
         // the threads' sums, then the warps'
-#pragma unroll
-        for (int o = 16; o; o >>= 1) q.join(far(q, o));
+        q.join_warp();
         if (lane == 0) {
             soft[0][warp] = q.m;
             soft[1][warp] = q.s.sum();
@@ -343,8 +359,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
             // NT / 32 is at most 8: the lanes behind hold nothing
             const bool some = tid < NT / 32;
             q = Soft{some ? soft[0][tid] : -INFINITY, F2(some ? soft[1][tid] : 0.0f, 0.0f), F2(some ? soft[2][tid] : 0.0f, 0.0f)};
-#pragma unroll
-            for (int o = 4; o; o >>= 1) q.join(far(q, o));
+            q.join_warp();
             if (tid == 0) {
                 mine[0] = q.m;
                 mine[1] = q.s.sum();
@@ -359,8 +374,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
                     const bool some = tid < C;
                     const float *there = cluster.map_shared_rank(mine, some ? tid : 0);
                     q = Soft{some ? there[0] : -INFINITY, F2(some ? there[1] : 0.0f, 0.0f), F2(some ? there[2] : 0.0f, 0.0f)};
-#pragma unroll
-                    for (int o = 4; o; o >>= 1) q.join(far(q, o));
+                    q.join_warp();
                 }
                 if (TOP) {
                     for (uint32_t i = tid + a.top; i < C * a.top; i += NT) {
