@@ -18,7 +18,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float FAR = -1e30f;             // exponents stop here: 2^FAR is 0, and FAR times 0 is 0, not NaN
 constexpr int PACKS = 4;                  // of 16 bytes, that a thread has of a piece
 constexpr uint32_t FOUND = 512;           // candidates that a block can hold
-constexpr uint32_t DEPTH = 4;             // pieces that a warp asks for ahead
+constexpr uint32_t DEPTH = 3;             // pieces that a warp asks for ahead
 constexpr uint32_t PIECE_BYTES = 32 * PACKS * 16;      // of a warp
 
 __device__ __forceinline__ float ex2(float x) {
@@ -124,7 +124,7 @@ __device__ __forceinline__ float top_of<__half>(const Pack<__half, 8> &p) {
 struct Found {
     uint64_t key[FOUND];
     uint64_t best[HE_MAX_TOP];
-    uint32_t count, bound[8], from;          // from: order of what a candidate has at least
+    uint32_t count, bound[8];
     uint64_t most[8];
 };
 
@@ -160,21 +160,6 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
     uint32_t low = f.bound[0];
     for (uint32_t i = 1; i < warps; i++) low = min(low, f.bound[i]);
     return low;
-}
-
-// Raises the bound to the top-th of the candidates that are there; by a warp, while others add to them (a place that is not written yet is 0).
-__device__ __forceinline__ void raise_bound(Found &f, uint32_t top) {
-    __syncwarp();
-    const uint32_t n = min(*(volatile uint32_t *)&f.count, FOUND);
-    if (n < top) return;
-    for (uint32_t i = threadIdx.x & 31u; i < n; i += 32) {
-        const uint64_t mine = *(volatile uint64_t *)&f.key[i];
-        uint32_t above = 0;
-#pragma unroll 8
-        for (uint32_t j = 0; j < n; j++) above += f.key[j] > mine;
-        if (mine && above == top - 1) atomicMax(&f.from, (uint32_t)(mine >> 32));
-    }
-    __syncwarp();
 }
 
 // The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are as high as the
@@ -218,8 +203,7 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
 // Rows by clusters of C blocks (C = 1: by blocks), which take a row's pieces in turn; each warp has its part of a piece, PIECE_BYTES in a row, and
 // asks for its parts by bulk copies, DEPTH ahead and on into the next row (asked for in registers, one ahead: 307 us for 2048 x
 // 131072 in bf16 with eight alternatives; so 193).  Candidates for the alternatives are values that are not below a bound on the top-th value,
-// which the warps raise in turn after 1, 2, 4, ... pieces, in which about as many candidates come as are wanted; they do not wait for one another
-// (with the candidates cut down by the whole block each time: 180 us, without alternatives 127).
+// raised after 1, 4, 16, ... pieces, between which some three times as many candidates come as are wanted.
 template <class T, bool TOP>
 __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C, int *status) {
     constexpr int V = WIDE<T>;
@@ -275,9 +259,11 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         uint32_t held = 0, round = 0;
         // vectors that lie in the row as a whole
         const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V;
+        float from = -INFINITY;              // what a candidate has at least
+        uint32_t raise = 0;                  // the piece after which the bound is raised next
+        bool lost = false;
         if (TOP) {
-            for (uint32_t i = tid; i < FOUND; i += NT) f.key[i] = 0;
-            if (tid == 0) f.count = f.from = 0;
+            if (tid == 0) f.count = 0;
             __syncthreads();
         }
         for (uint32_t c = rank; c < pieces; c += C, round++) {
@@ -314,14 +300,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
 #pragma unroll
                 for (int e = 0; e < V; e += 2) q.add(F2(to_f32(z[i].v[e]), to_f32(z[i].v[e + 1])), b);
             if (TOP) {
-                if (round == 0) {
-                    const uint32_t bound = bound_of_top(f, order_of(m), a.top);
-                    if (lane == 0) atomicMax(&f.from, bound);
-                    __syncwarp();
-                } else if ((round & (round - 1)) == 0 && __clz((int)round) % (NT / 32) == warp) {
-                    raise_bound(f, a.top);
-                }
-                const float from = value_of(*(volatile uint32_t *)&f.from);
+                if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
                 // threads that have a candidate, few: the warp looks through the values of one after the other, a lane at each value
                 for (uint32_t who = __ballot_sync(0xffffffffu, m >= from); who; who &= who - 1) {
                     const uint32_t l = __ffs(who) - 1, i = lane / V, e = lane % V;
@@ -336,17 +315,24 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
                     if (hit && at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
                     __syncwarp();
                 }
+                if (round == raise || c + C >= pieces) {
+                    raise = raise * 4 + 3;
+                    __syncthreads();
+                    const uint32_t found = f.count;
+                    __syncthreads();
+                    lost |= found > FOUND;
+                    held = keep_best(f, min(found, FOUND), a.top);
+                    // later pieces have higher indices: with enough candidates a value equal to the lowest of them is too late
+                    if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.key[a.top - 1] >> 32) + 1));
+                    __syncthreads();
+                }
             }
             __syncwarp();
             if (lane == 0) ask(d);
             if (++d == DEPTH) d = 0, turn ^= 1u;
         }
-        if (TOP) {
-            __syncthreads();
-            const uint32_t found = f.count;
-            // too many candidates; or too few, where NaN is among the row's highest
-            held = found < a.top || found > FOUND ? search<T>(f, row, rank, C, pieces, a.top) : keep_best(f, found, a.top);
-        }
+        // too many candidates; or too few, where NaN is among the row's highest
+        if (TOP && (lost || held < a.top)) held = search<T>(f, row, rank, C, pieces, a.top);
         // the threads' sums, then the warps'
         q.join_warp();
         if (lane == 0) {
@@ -420,15 +406,17 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
     if (gone) copies_lost(status);
 }
 
-// Threads of a block: as few as hold a row of up to 256 threads' packs at once.
-inline uint32_t row_threads(size_t bytes) {
-    const size_t t = (bytes + 15 + PACKS * 16 - 1) / (PACKS * 16);
-    return t >= 256 ? 256 : (uint32_t)(t + 31) / 32 * 32;
+// Threads of a block: as few as hold a row at once, up to 128, of which an SM has six blocks, so that one's barriers and searches are hidden by the
+// others (2048 x 131072 with eight alternatives: 256 threads 189 us, 128 151, 64 190); up to 256 where there are fewer rows than SMs (one row: 14.4
+// and 23.2 us).
+inline uint32_t row_threads(size_t bytes, size_t rows, int n_sm) {
+    const size_t t = (bytes + 15 + PACKS * 16 - 1) / (PACKS * 16), most = rows < (size_t)n_sm ? 256 : 128;
+    return t >= most ? (uint32_t)most : (uint32_t)(t + 31) / 32 * 32;
 }
 
 template <class T>
 cudaError_t log_probs_of(const LogProbsArgs &a, int n_sm, int *status, cudaStream_t s) {
-    const uint32_t nt = row_threads(a.vocab * sizeof(T));
+    const uint32_t nt = row_threads(a.vocab * sizeof(T), a.rows, n_sm);
     const size_t pieces = (a.vocab * sizeof(T) + 15 + (size_t)nt * PACKS * 16 - 1) / ((size_t)nt * PACKS * 16);
     const uint32_t bytes = nt / 32 * DEPTH * PIECE_BYTES;
     // blocks that an SM holds: 768 threads by the registers, and shared memory
