@@ -41,7 +41,7 @@ struct LogProbsGradArgs {
     const float *dtop;
     MatOut dlogits;
 };
-cudaError_t launch_log_probs_grad(const LogProbsGradArgs &a, int dtype, int n_sm, cudaStream_t s);
+cudaError_t launch_log_probs_grad(const LogProbsGradArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
 struct NormArgs {
     MatArg x;

@@ -59,7 +59,7 @@ int he_token_log_probs_backward(he_ctx *ctx, const void *logits_dev, int dtype, 
     if (logits_dev == dlogits_dev && rows > 1 && row_stride != dlogits_stride) return HE_ERR_INVALID_ARG;
     const LogProbsGradArgs a{{logits_dev, row_stride}, rows, vocab, targets_dev, lse_dev, entropy_dev, dlogp_dev, dentropy_dev, top, top_ids_dev, dtop_dev,
                              {dlogits_dev, dlogits_stride}};
-    return done(launch_log_probs_grad(a, dtype, ctx->sm_count, as_stream(stream)));
+    return done(launch_log_probs_grad(a, dtype, ctx->sm_count, ctx->dev.status, as_stream(stream)));
 }
 
 int he_layer_norm(he_ctx *ctx, const void *x_dev, int dtype, size_t rows, size_t width, size_t x_stride, const void *weight_dev,

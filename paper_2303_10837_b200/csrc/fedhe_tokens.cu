@@ -449,76 +449,167 @@ cudaError_t log_probs_of(const LogProbsArgs &a, int n_sm, int *status, cudaStrea
 
 // ---------------------------------------------------------------------------
 
-// One row's part [v0, v1) of vectors by a block.  The elements that a gradient falls on by itself (the target, the alternatives) are computed
-// first, from logits that the result may replace, and written last.
-template <class T>
-__global__ void __launch_bounds__(256) log_probs_grad_kernel(const LogProbsGradArgs a, const uint32_t parts) {
-    constexpr int V = WIDE<T>, NV = 4;
-    const uint32_t tid = threadIdx.x, NT = blockDim.x, part = blockIdx.x % parts;
-    const size_t r = blockIdx.x / parts;
-    const Row<T> row(static_cast<const T *>(a.logits.p) + r * a.logits.stride, (uint32_t)a.vocab);
-    T *out = static_cast<T *>(a.dlogits.p) + r * a.dlogits.stride;
-    const uint32_t v0 = (uint32_t)((uint64_t)row.vectors * part / parts), v1 = (uint32_t)((uint64_t)row.vectors * (part + 1) / parts);
-    const int64_t y = a.targets[r];
-    const float lse = a.lse[r], gh = a.dentropy ? a.dentropy[r] : 0.0f, H = a.dentropy ? a.entropy[r] : 0.0f;
-    const float gy = y < 0 ? 0.0f : y < (int64_t)row.n ? a.dlogp[r] : NAN;
-    float G = gy;
-    for (uint32_t i = 0; i < a.top; i++) G += a.dtop[r * a.top + i];
-    // nothing flows into the row, or every logit of it is -inf: what it holds does not count
-    const bool still = lse == -INFINITY || (y < 0 && !a.dentropy && !a.top);
-    const auto grad = [&](float z) {
-        const float lp = max_nan(z - lse, FAR), p = ex2(lp * LOG2E);
-        return -p * fmaf(gh, lp + H, G);
+// What flows into a row.
+struct Flow {
+    int64_t y;
+    float lse, gy, G, gh, H;                 // gradients of the target's log probability, of all log probabilities, of the entropy; the entropy
+    bool still;                              // nothing flows, or every logit is -inf: whatever the row holds, zeros come out
+};
+
+// Warps take parts of rows, PIECE_BYTES each, in turn, and ask for them by bulk copies, GRAD_DEPTH ahead; a part needs nothing but its row's
+// numbers, so no warp waits for another.  The elements that a gradient falls on by itself (the target, the alternatives) get it before the one rounding.
+constexpr uint32_t GRAD_THREADS = 128, GRAD_DEPTH = 4;
+template <class T, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(GRAD_THREADS, 6) log_probs_grad_kernel(const LogProbsGradArgs a, const uint32_t pieces, int *status) {
+    constexpr int V = WIDE<T>;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ uint64_t bars[GRAD_THREADS / 32][GRAD_DEPTH];
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31u, rows = (uint32_t)a.rows, n = (uint32_t)a.vocab;
+    const uint32_t warps = gridDim.x * (GRAD_THREADS / 32), me = blockIdx.x * (GRAD_THREADS / 32) + warp;
+    const uint32_t rows_on = warps / pieces, pieces_on = warps % pieces;       // from a warp's part to its next one
+    const size_t pitch = a.logits.stride * sizeof(T);
+    const uintptr_t base = reinterpret_cast<uintptr_t>(a.logits.p);
+    const uintptr_t low = (base + 15) & ~(uintptr_t)15, high = (base + (rows - 1) * pitch + (size_t)n * sizeof(T)) & ~(uintptr_t)15;
+    uint8_t *room = ring + warp * GRAD_DEPTH * PIECE_BYTES;
+    const uint32_t room_at = shared_at(room), bar = shared_at(&bars[warp][0]);
+    const auto on = [&](uint32_t &row, uint32_t &piece) {
+        row += rows_on;
+        piece += pieces_on;
+        if (piece >= pieces) piece -= pieces, row++;
     };
-    float own = 0.0f;
-    int64_t at = -1;
-    if (!still && tid <= a.top) {
-        at = tid == a.top ? y : a.top_ids[r * a.top + tid];
-        if (at < 0 || at >= (int64_t)row.n || at < row.first(v0) || at >= row.first(v1)) at = -1;
-        if (at >= 0) {
-            float g = at == y ? gy : 0.0f;
-            for (uint32_t i = 0; i < a.top; i++)
-                if (a.top_ids[r * a.top + i] == at) g += a.dtop[r * a.top + i];
-            own = g + grad(to_f32(row.p[at]));
-        }
+    uint32_t asked_row = me / pieces, asked = me % pieces;
+    const auto ask = [&](uint32_t d) {
+        if (asked_row >= rows) return;
+        const uintptr_t row = base + asked_row * pitch, from = (row & ~(uintptr_t)15) + (size_t)asked * PIECE_BYTES;
+        uintptr_t end = (row + (size_t)n * sizeof(T) + 15) & ~(uintptr_t)15;
+        end = end < high ? end : high;
+        const uintptr_t at = from < low ? low : from, to = from + PIECE_BYTES < end ? from + PIECE_BYTES : end;
+        const uint32_t bytes = to > at ? (uint32_t)(to - at) : 0;
+        copies_begin(bar + d * 8, bytes);
+        if (bytes) bulk_copy(room_at + d * PIECE_BYTES + (uint32_t)(at - from), at, bytes, bar + d * 8);
+        on(asked_row, asked);
+    };
+    const auto flow_of = [&](uint32_t r) {
+        Flow f;
+        f.y = a.targets[r];
+        f.lse = a.lse[r];
+        f.gy = f.y < 0 ? 0.0f : f.y < (int64_t)n ? a.dlogp[r] : NAN;
+        f.G = f.gy;
+        f.gh = ENTROPY ? a.dentropy[r] : 0.0f;
+        f.H = ENTROPY ? a.entropy[r] : 0.0f;
+        f.still = f.lse == -INFINITY || (f.y < 0 && !ENTROPY && !TOP);
+        return f;
+    };
+    if (lane == 0) {
+        for (uint32_t d = 0; d < GRAD_DEPTH; d++) barrier_init(bar + d * 8, 1);
+        barriers_ready();
+        for (uint32_t d = 0; d < GRAD_DEPTH; d++) ask(d);
     }
-    __syncthreads();
-    const bool alike = ((reinterpret_cast<uintptr_t>(row.p) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
-    for (uint32_t c = v0 + tid; c < v1; c += NT * NV) {
-        Pack<T, V> z[NV];
+    uint32_t r = me / pieces, piece = me % pieces, d = 0, turn = 0;
+    bool gone = false;
+    Flow next;
+    if (r < rows) next = flow_of(r);
+    __syncwarp();
+    while (r < rows) {
+        Flow f = next;
+        const Row<T> row(reinterpret_cast<const T *>(base + r * pitch), n);
+        T *out = static_cast<T *>(a.dlogits.p) + (size_t)r * a.dlogits.stride;
+        const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V, v0 = piece * (32 * PACKS);
+        const bool inside = v0 >= whole_from && v0 + 32 * PACKS <= whole_to;
+        const bool alike = ((reinterpret_cast<uintptr_t>(row.p) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+        uint32_t r_next = r, piece_next = piece;
+        on(r_next, piece_next);
+        if (r_next < rows) next = flow_of(r_next);
+        // whether the target or an alternative lies in this part
+        const int64_t first = row.first(v0), behind = first + 32 * PACKS * V;
+        bool hit = f.y >= first && f.y < behind;
+        if (TOP) {
+            float sum = 0.0f;
+            for (uint32_t i = lane; i < a.top; i += 32) {
+                const int64_t id = a.top_ids[(size_t)r * a.top + i];
+                sum += a.dtop[(size_t)r * a.top + i];
+                hit = hit || (id >= first && id < behind);
+            }
+            f.G += warp_sum(sum);
+            hit = __any_sync(0xffffffffu, hit);
+        }
+        if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
+        const uint8_t *in = room + d * PIECE_BYTES + lane * 16;
+        Pack<T, V> z[PACKS];
 #pragma unroll
-        for (int i = 0; i < NV; i++)
-            if (!still && c + i * NT < v1) z[i] = row.load(c + i * NT);
+        for (int i = 0; i < PACKS; i++) {
+            const uint32_t v = v0 + i * 32 + lane;
+            if (inside || (v >= whole_from && v < whole_to)) z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in + i * 512));
+            else if (v < row.vectors) z[i] = row.load(v);
+            else
 #pragma unroll
-        for (int i = 0; i < NV; i++) {
-            const uint32_t v = c + i * NT;
-            if (v >= v1) break;
-            Pack<T, V> d;
+                for (int e = 0; e < V; e++) z[i].v[e] = from_f32<T>(0.0f);
+        }
+        __syncwarp();
+        if (lane == 0) ask(d);
+        if (++d == GRAD_DEPTH) d = 0, turn ^= 1u;
 #pragma unroll
-            for (int e = 0; e < V; e++) d.v[e] = from_f32<T>(still ? 0.0f : grad(to_f32(z[i].v[e])));
-            if (alike && row.whole(v)) {
-                store_pack<T, V>(out + row.first(v), d);
-            } else {
+        for (int i = 0; i < PACKS; i++) {
+            const uint32_t v = v0 + i * 32 + lane;
+            F2 g[V / 2];
+#pragma unroll
+            for (int e = 0; e < V / 2; e++) {
+                const F2 l = F2(to_f32(z[i].v[2 * e]), to_f32(z[i].v[2 * e + 1])) + F2(-f.lse);
+                if (ENTROPY) {
+                    float2 lp = l.both();
+                    lp.x = max_nan(lp.x, FAR);
+                    lp.y = max_nan(lp.y, FAR);
+                    const float2 t = (F2(lp.x, lp.y) * F2(LOG2E)).both();
+                    g[e] = F2(-ex2(t.x), -ex2(t.y)) * fma2(F2(f.gh), F2(lp.x, lp.y) + F2(f.H), F2(f.G));
+                } else {
+                    const float2 t = (l * F2(LOG2E)).both();
+                    g[e] = F2(ex2(t.x), ex2(t.y)) * F2(-f.G);
+                }
+            }
+            if (hit) {
+                const int64_t j = row.first(v);
+#pragma unroll
+                for (int e = 0; e < V; e++) {
+                    float more = j + e == f.y ? f.gy : 0.0f;
+                    if (TOP)
+                        for (uint32_t k = 0; k < a.top; k++)
+                            if (a.top_ids[(size_t)r * a.top + k] == j + e) more += a.dtop[(size_t)r * a.top + k];
+                    g[e / 2] = g[e / 2] + (e % 2 ? F2(0.0f, more) : F2(more, 0.0f));
+                }
+            }
+            Pack<T, V> o;
+#pragma unroll
+            for (int e = 0; e < V / 2; e++) {
+                const float2 x = g[e].both();
+                o.v[2 * e] = from_f32<T>(f.still ? 0.0f : x.x);
+                o.v[2 * e + 1] = from_f32<T>(f.still ? 0.0f : x.y);
+            }
+            if (alike && (inside || (v >= whole_from && v < whole_to))) {
+                store_pack<T, V>(out + row.first(v), o);
+            } else if (v < row.vectors) {
 #pragma unroll
                 for (int e = 0; e < V; e++) {
                     const int64_t j = row.first(v) + e;
-                    if (j >= 0 && j < (int64_t)row.n) out[j] = d.v[e];
+                    if (j >= 0 && j < (int64_t)row.n) out[j] = o.v[e];
                 }
             }
         }
+        r = r_next;
+        piece = piece_next;
     }
-    __syncthreads();
-    if (at >= 0) out[at] = from_f32<T>(own);
+    if (gone) copies_lost(status);
 }
 
 template <class T>
-cudaError_t log_probs_grad_of(const LogProbsGradArgs &a, int n_sm, cudaStream_t s) {
-    const size_t vectors = a.vocab / WIDE<T> + 2;
-    const uint32_t nt = 256;
-    size_t parts = (vectors + nt * 4 - 1) / (nt * 4);
-    const size_t wanted = ((size_t)8 * n_sm + a.rows - 1) / a.rows;
-    if (parts > wanted) parts = wanted;
-    log_probs_grad_kernel<T><<<(unsigned)(a.rows * parts), nt, 0, s>>>(a, (uint32_t)parts);
+cudaError_t log_probs_grad_of(const LogProbsGradArgs &a, int n_sm, int *status, cudaStream_t s) {
+    const uint32_t pieces = (uint32_t)((a.vocab * sizeof(T) + 15 + PIECE_BYTES - 1) / PIECE_BYTES), bytes = GRAD_THREADS / 32 * GRAD_DEPTH * PIECE_BYTES;
+    const size_t blocks = (a.rows * pieces + GRAD_THREADS / 32 - 1) / (GRAD_THREADS / 32), most = (size_t)6 * n_sm;
+    const auto kernel = a.top           ? (a.dentropy ? log_probs_grad_kernel<T, true, true> : log_probs_grad_kernel<T, false, true>)
+                        : a.dentropy    ? log_probs_grad_kernel<T, true, false>
+                                        : log_probs_grad_kernel<T, false, false>;
+    const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (rc != cudaSuccess) return rc;
+    kernel<<<(unsigned)(blocks < most ? blocks : most), GRAD_THREADS, bytes, s>>>(a, pieces, status);
     return FEDHE_LAUNCHED();
 }
 
@@ -530,10 +621,10 @@ cudaError_t launch_log_probs(const LogProbsArgs &a, int dtype, int n_sm, int *st
                               : log_probs_of<__half>(a, n_sm, status, s);
 }
 
-cudaError_t launch_log_probs_grad(const LogProbsGradArgs &a, int dtype, int n_sm, cudaStream_t s) {
-    return dtype == HE_F32    ? log_probs_grad_of<float>(a, n_sm, s)
-           : dtype == HE_BF16 ? log_probs_grad_of<__nv_bfloat16>(a, n_sm, s)
-                              : log_probs_grad_of<__half>(a, n_sm, s);
+cudaError_t launch_log_probs_grad(const LogProbsGradArgs &a, int dtype, int n_sm, int *status, cudaStream_t s) {
+    return dtype == HE_F32    ? log_probs_grad_of<float>(a, n_sm, status, s)
+           : dtype == HE_BF16 ? log_probs_grad_of<__nv_bfloat16>(a, n_sm, status, s)
+                              : log_probs_grad_of<__half>(a, n_sm, status, s);
 }
 
 }  // namespace fedhe
