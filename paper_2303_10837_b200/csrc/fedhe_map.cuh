@@ -90,6 +90,36 @@ __device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
     return r;
 }
 
+// Elements 2 i and 2 i + 1 of a pack, of more than one.
+template <class T, int V>
+__device__ __forceinline__ F2 two_of(const Pack<T, V> &p, int i) { return F2(to_f32(p.v[2 * i]), to_f32(p.v[2 * i + 1])); }
+template <int V>
+__device__ __forceinline__ F2 two_of(const Pack<__nv_bfloat16, V> &p, int i) {
+    const uint32_t w = reinterpret_cast<const uint32_t *>(&p)[i];
+    return F2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <int V>
+__device__ __forceinline__ F2 two_of(const Pack<__half, V> &p, int i) {
+    const float2 v = __half22float2(reinterpret_cast<const __half2 *>(&p)[i]);
+    return F2(v.x, v.y);
+}
+template <class T, int V>
+__device__ __forceinline__ void set_two(Pack<T, V> &p, int i, F2 x) {
+    const float2 v = x.both();
+    p.v[2 * i] = from_f32<T>(v.x);
+    p.v[2 * i + 1] = from_f32<T>(v.y);
+}
+template <int V>
+__device__ __forceinline__ void set_two(Pack<__nv_bfloat16, V> &p, int i, F2 x) {
+    const float2 v = x.both();
+    reinterpret_cast<__nv_bfloat162 *>(&p)[i] = __floats2bfloat162_rn(v.x, v.y);
+}
+template <int V>
+__device__ __forceinline__ void set_two(Pack<__half, V> &p, int i, F2 x) {
+    const float2 v = x.both();
+    reinterpret_cast<__half2 *>(&p)[i] = __floats2half2_rn(v.x, v.y);
+}
+
 // The larger one; NaN where one of them is.
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;

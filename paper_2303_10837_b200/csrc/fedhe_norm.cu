@@ -248,16 +248,23 @@ __device__ __forceinline__ void load_weights(F2 (&w)[K * V / 2], const void *p, 
 template <class T, int V, int K>
 __device__ __forceinline__ void pairs_of(F2 (&x)[K * V / 2], const Pack<T, V> (&p)[K]) {
 #pragma unroll
-    for (int i = 0; i < K * V; i += 2) x[i / 2] = F2(to_f32(p[i / V].v[i % V]), to_f32(p[(i + 1) / V].v[(i + 1) % V]));
+    for (int i = 0; i < K * V; i += 2) {
+        if constexpr (V > 1) x[i / 2] = two_of(p[i / V], i % V / 2);
+        else x[i / 2] = F2(to_f32(p[i].v[0]), to_f32(p[i + 1].v[0]));
+    }
 }
 template <class T, int V, int K>
 __device__ __forceinline__ void store_row(T *row, const F2 (&x)[K * V / 2], uint32_t t, uint32_t threads, uint32_t width) {
     Pack<T, V> o[K];
 #pragma unroll
     for (int i = 0; i < K * V; i += 2) {
-        const float2 v = x[i / 2].both();
-        o[i / V].v[i % V] = from_f32<T>(v.x);
-        o[(i + 1) / V].v[(i + 1) % V] = from_f32<T>(v.y);
+        if constexpr (V > 1) {
+            set_two(o[i / V], i % V / 2, x[i / 2]);
+        } else {
+            const float2 v = x[i / 2].both();
+            o[i].v[0] = from_f32<T>(v.x);
+            o[i + 1].v[0] = from_f32<T>(v.y);
+        }
     }
 #pragma unroll
     for (int k = 0; k < K; k++) {

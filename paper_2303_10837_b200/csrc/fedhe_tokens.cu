@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
 #pragma unroll
             for (int i = 0; i < PACKS; i++)
 #pragma unroll
-                for (int e = 0; e < V; e += 2) q.add(F2(to_f32(z[i].v[e]), to_f32(z[i].v[e + 1])), b);
+                for (int e = 0; e < V / 2; e++) q.add(two_of(z[i], e), b);
             if (TOP) {
                 if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
                 // threads that have a candidate, few: the warp looks through the values of one after the other, a lane at each value
@@ -456,38 +456,47 @@ struct Flow {
     bool still;                              // nothing flows, or every logit is -inf: whatever the row holds, zeros come out
 };
 
-// Warps take parts of rows, PIECE_BYTES each, in turn, and ask for them by bulk copies, GRAD_DEPTH ahead; a part needs nothing but its row's
-// numbers, so no warp waits for another.  The elements that a gradient falls on by itself (the target, the alternatives) get it before the one rounding.
+// Warps take parts of rows in turn, `run` pieces of PIECE_BYTES each, and ask for the pieces by bulk copies, GRAD_DEPTH ahead; a part needs nothing but
+// its row's numbers, so no warp waits for another.  The elements that a gradient falls on by itself (the target, the alternatives) get it before the one rounding.
 constexpr uint32_t GRAD_THREADS = 128, GRAD_DEPTH = 4;
 template <class T, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(GRAD_THREADS, 6) log_probs_grad_kernel(const LogProbsGradArgs a, const uint32_t pieces, int *status) {
+__global__ void __launch_bounds__(GRAD_THREADS, 6) log_probs_grad_kernel(const LogProbsGradArgs a, const uint32_t pieces, const uint32_t run, int *status) {
     constexpr int V = WIDE<T>;
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ uint64_t bars[GRAD_THREADS / 32][GRAD_DEPTH];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31u, rows = (uint32_t)a.rows, n = (uint32_t)a.vocab;
     const uint32_t warps = gridDim.x * (GRAD_THREADS / 32), me = blockIdx.x * (GRAD_THREADS / 32) + warp;
-    const uint32_t rows_on = warps / pieces, pieces_on = warps % pieces;       // from a warp's part to its next one
+    const uint32_t parts = (pieces + run - 1) / run, rows_on = warps / parts, parts_on = warps % parts;       // from a warp's part to its next one
     const size_t pitch = a.logits.stride * sizeof(T);
     const uintptr_t base = reinterpret_cast<uintptr_t>(a.logits.p);
     const uintptr_t low = (base + 15) & ~(uintptr_t)15, high = (base + (rows - 1) * pitch + (size_t)n * sizeof(T)) & ~(uintptr_t)15;
     uint8_t *room = ring + warp * GRAD_DEPTH * PIECE_BYTES;
     const uint32_t room_at = shared_at(room), bar = shared_at(&bars[warp][0]);
-    const auto on = [&](uint32_t &row, uint32_t &piece) {
+    const auto on = [&](uint32_t &row, uint32_t &part) {
         row += rows_on;
-        piece += pieces_on;
-        if (piece >= pieces) piece -= pieces, row++;
+        part += parts_on;
+        if (part >= parts) part -= parts, row++;
     };
-    uint32_t asked_row = me / pieces, asked = me % pieces;
+    uint32_t asked_row = me / parts, asked = me % parts, asked_left = 0;       // by the first lane: the part whose pieces are asked for
+    uintptr_t asked_at = 0, asked_end = 0;
+    const auto enter = [&] {
+        const uintptr_t row = base + asked_row * pitch;
+        asked_at = (row & ~(uintptr_t)15) + (size_t)asked * run * PIECE_BYTES;
+        asked_end = (row + (size_t)n * sizeof(T) + 15) & ~(uintptr_t)15;
+        if (asked_end > high) asked_end = high;
+        asked_left = min(run, pieces - asked * run);
+    };
     const auto ask = [&](uint32_t d) {
         if (asked_row >= rows) return;
-        const uintptr_t row = base + asked_row * pitch, from = (row & ~(uintptr_t)15) + (size_t)asked * PIECE_BYTES;
-        uintptr_t end = (row + (size_t)n * sizeof(T) + 15) & ~(uintptr_t)15;
-        end = end < high ? end : high;
-        const uintptr_t at = from < low ? low : from, to = from + PIECE_BYTES < end ? from + PIECE_BYTES : end;
+        const uintptr_t at = asked_at < low ? low : asked_at, to = asked_at + PIECE_BYTES < asked_end ? asked_at + PIECE_BYTES : asked_end;
         const uint32_t bytes = to > at ? (uint32_t)(to - at) : 0;
         copies_begin(bar + d * 8, bytes);
-        if (bytes) bulk_copy(room_at + d * PIECE_BYTES + (uint32_t)(at - from), at, bytes, bar + d * 8);
-        on(asked_row, asked);
+        if (bytes) bulk_copy(room_at + d * PIECE_BYTES + (uint32_t)(at - asked_at), at, bytes, bar + d * 8);
+        asked_at += PIECE_BYTES;
+        if (--asked_left == 0) {
+            on(asked_row, asked);
+            enter();
+        }
     };
     const auto flow_of = [&](uint32_t r) {
         Flow f;
@@ -503,9 +512,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 6) log_probs_grad_kernel(const L
     if (lane == 0) {
         for (uint32_t d = 0; d < GRAD_DEPTH; d++) barrier_init(bar + d * 8, 1);
         barriers_ready();
+        enter();
         for (uint32_t d = 0; d < GRAD_DEPTH; d++) ask(d);
     }
-    uint32_t r = me / pieces, piece = me % pieces, d = 0, turn = 0;
+    uint32_t r = me / parts, part = me % parts, d = 0, turn = 0;
     bool gone = false;
     Flow next;
     if (r < rows) next = flow_of(r);
@@ -514,88 +524,94 @@ __global__ void __launch_bounds__(GRAD_THREADS, 6) log_probs_grad_kernel(const L
         Flow f = next;
         const Row<T> row(reinterpret_cast<const T *>(base + r * pitch), n);
         T *out = static_cast<T *>(a.dlogits.p) + (size_t)r * a.dlogits.stride;
-        const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V, v0 = piece * (32 * PACKS);
-        const bool inside = v0 >= whole_from && v0 + 32 * PACKS <= whole_to;
+        const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V;
         const bool alike = ((reinterpret_cast<uintptr_t>(row.p) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
-        uint32_t r_next = r, piece_next = piece;
-        on(r_next, piece_next);
+        uint32_t r_next = r, part_next = part;
+        on(r_next, part_next);
         if (r_next < rows) next = flow_of(r_next);
-        // whether the target or an alternative lies in this part
-        const int64_t first = row.first(v0), behind = first + 32 * PACKS * V;
-        bool hit = f.y >= first && f.y < behind;
         if (TOP) {
             float sum = 0.0f;
-            for (uint32_t i = lane; i < a.top; i += 32) {
-                const int64_t id = a.top_ids[(size_t)r * a.top + i];
-                sum += a.dtop[(size_t)r * a.top + i];
-                hit = hit || (id >= first && id < behind);
-            }
+            for (uint32_t i = lane; i < a.top; i += 32) sum += a.dtop[(size_t)r * a.top + i];
             f.G += warp_sum(sum);
-            hit = __any_sync(0xffffffffu, hit);
         }
-        if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
-        const uint8_t *in = room + d * PIECE_BYTES + lane * 16;
-        Pack<T, V> z[PACKS];
+        const uint32_t to = min(part * run + run, pieces) * (32 * PACKS);
+        for (uint32_t v0 = part * run * (32 * PACKS); v0 < to; v0 += 32 * PACKS) {
+            const bool inside = v0 >= whole_from && v0 + 32 * PACKS <= whole_to;
+            // whether the target or an alternative lies in this piece
+            const int64_t first = row.first(v0), behind = first + 32 * PACKS * V;
+            bool hit = f.y >= first && f.y < behind;
+            if (TOP) {
+                for (uint32_t i = lane; i < a.top; i += 32) {
+                    const int64_t id = a.top_ids[(size_t)r * a.top + i];
+                    hit = hit || (id >= first && id < behind);
+                }
+                hit = __any_sync(0xffffffffu, hit);
+            }
+            if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
+            const uint8_t *in = room + d * PIECE_BYTES + lane * 16;
+            Pack<T, V> z[PACKS];
+            if (inside) {
 #pragma unroll
-        for (int i = 0; i < PACKS; i++) {
-            const uint32_t v = v0 + i * 32 + lane;
-            if (inside || (v >= whole_from && v < whole_to)) z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in + i * 512));
-            else if (v < row.vectors) z[i] = row.load(v);
-            else
+                for (int i = 0; i < PACKS; i++) z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in + i * 512));
+            } else {
 #pragma unroll
-                for (int e = 0; e < V; e++) z[i].v[e] = from_f32<T>(0.0f);
-        }
-        __syncwarp();
-        if (lane == 0) ask(d);
-        if (++d == GRAD_DEPTH) d = 0, turn ^= 1u;
+                for (int i = 0; i < PACKS; i++) {
+                    const uint32_t v = v0 + i * 32 + lane;
+                    if (v >= whole_from && v < whole_to) z[i] = load_pack<T, V>(reinterpret_cast<const T *>(in + i * 512));
+                    else if (v < row.vectors) z[i] = row.load(v);
+                    else
 #pragma unroll
-        for (int i = 0; i < PACKS; i++) {
-            const uint32_t v = v0 + i * 32 + lane;
-            F2 g[V / 2];
-#pragma unroll
-            for (int e = 0; e < V / 2; e++) {
-                const F2 l = F2(to_f32(z[i].v[2 * e]), to_f32(z[i].v[2 * e + 1])) + F2(-f.lse);
-                if (ENTROPY) {
-                    float2 lp = l.both();
-                    lp.x = max_nan(lp.x, FAR);
-                    lp.y = max_nan(lp.y, FAR);
-                    const float2 t = (F2(lp.x, lp.y) * F2(LOG2E)).both();
-                    g[e] = F2(-ex2(t.x), -ex2(t.y)) * fma2(F2(f.gh), F2(lp.x, lp.y) + F2(f.H), F2(f.G));
-                } else {
-                    const float2 t = (l * F2(LOG2E)).both();
-                    g[e] = F2(ex2(t.x), ex2(t.y)) * F2(-f.G);
+                        for (int e = 0; e < V; e++) z[i].v[e] = from_f32<T>(0.0f);
                 }
             }
-            if (hit) {
-                const int64_t j = row.first(v);
+            __syncwarp();
+            if (lane == 0) ask(d);
+            if (++d == GRAD_DEPTH) d = 0, turn ^= 1u;
 #pragma unroll
-                for (int e = 0; e < V; e++) {
-                    float more = j + e == f.y ? f.gy : 0.0f;
-                    if (TOP)
-                        for (uint32_t k = 0; k < a.top; k++)
-                            if (a.top_ids[(size_t)r * a.top + k] == j + e) more += a.dtop[(size_t)r * a.top + k];
-                    g[e / 2] = g[e / 2] + (e % 2 ? F2(0.0f, more) : F2(more, 0.0f));
+            for (int i = 0; i < PACKS; i++) {
+                const uint32_t v = v0 + i * 32 + lane;
+                F2 g[V / 2];
+#pragma unroll
+                for (int e = 0; e < V / 2; e++) {
+                    const F2 l = two_of(z[i], e) + F2(-f.lse);
+                    if (ENTROPY) {
+                        float2 lp = l.both();
+                        lp.x = max_nan(lp.x, FAR);
+                        lp.y = max_nan(lp.y, FAR);
+                        const float2 t = (F2(lp.x, lp.y) * F2(LOG2E)).both();
+                        g[e] = F2(-ex2(t.x), -ex2(t.y)) * fma2(F2(f.gh), F2(lp.x, lp.y) + F2(f.H), F2(f.G));
+                    } else {
+                        const float2 t = (l * F2(LOG2E)).both();
+                        g[e] = F2(ex2(t.x), ex2(t.y)) * F2(-f.G);
+                    }
+                }
+                if (hit) {
+                    const int64_t j = row.first(v);
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        float more = j + e == f.y ? f.gy : 0.0f;
+                        if (TOP)
+                            for (uint32_t k = 0; k < a.top; k++)
+                                if (a.top_ids[(size_t)r * a.top + k] == j + e) more += a.dtop[(size_t)r * a.top + k];
+                        g[e / 2] = g[e / 2] + (e % 2 ? F2(0.0f, more) : F2(more, 0.0f));
+                    }
+                }
+                Pack<T, V> o;
+#pragma unroll
+                for (int e = 0; e < V / 2; e++) set_two(o, e, f.still ? F2(0.0f) : g[e]);
+                if (alike && (inside || (v >= whole_from && v < whole_to))) {
+                    store_pack<T, V>(out + row.first(v), o);
+                } else if (v < row.vectors) {
+#pragma unroll
+                    for (int e = 0; e < V; e++) {
+                        const int64_t j = row.first(v) + e;
+                        if (j >= 0 && j < (int64_t)row.n) out[j] = o.v[e];
+                    }
                 }
             }
-            Pack<T, V> o;
-#pragma unroll
-            for (int e = 0; e < V / 2; e++) {
-                const float2 x = g[e].both();
-                o.v[2 * e] = from_f32<T>(f.still ? 0.0f : x.x);
-                o.v[2 * e + 1] = from_f32<T>(f.still ? 0.0f : x.y);
-            }
-            if (alike && (inside || (v >= whole_from && v < whole_to))) {
-                store_pack<T, V>(out + row.first(v), o);
-            } else if (v < row.vectors) {
-#pragma unroll
-                for (int e = 0; e < V; e++) {
-                    const int64_t j = row.first(v) + e;
-                    if (j >= 0 && j < (int64_t)row.n) out[j] = o.v[e];
-                }
-            }
-        }
+    }
         r = r_next;
-        piece = piece_next;
+        part = part_next;
     }
     if (gone) copies_lost(status);
 }
@@ -603,13 +619,17 @@ __global__ void __launch_bounds__(GRAD_THREADS, 6) log_probs_grad_kernel(const L
 template <class T>
 cudaError_t log_probs_grad_of(const LogProbsGradArgs &a, int n_sm, int *status, cudaStream_t s) {
     const uint32_t pieces = (uint32_t)((a.vocab * sizeof(T) + 15 + PIECE_BYTES - 1) / PIECE_BYTES), bytes = GRAD_THREADS / 32 * GRAD_DEPTH * PIECE_BYTES;
-    const size_t blocks = (a.rows * pieces + GRAD_THREADS / 32 - 1) / (GRAD_THREADS / 32), most = (size_t)6 * n_sm;
+    // parts of rows: up to sixteen pieces, as long as there are four parts for each warp
+    const size_t most = (size_t)6 * n_sm, warps = most * GRAD_THREADS / 32;
+    uint32_t run = 16;
+    while (run > 1 && a.rows * ((pieces + run - 1) / run) < 4 * warps) run /= 2;
+    const size_t blocks = (a.rows * ((pieces + run - 1) / run) + GRAD_THREADS / 32 - 1) / (GRAD_THREADS / 32);
     const auto kernel = a.top           ? (a.dentropy ? log_probs_grad_kernel<T, true, true> : log_probs_grad_kernel<T, false, true>)
                         : a.dentropy    ? log_probs_grad_kernel<T, true, false>
                                         : log_probs_grad_kernel<T, false, false>;
     const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (rc != cudaSuccess) return rc;
-    kernel<<<(unsigned)(blocks < most ? blocks : most), GRAD_THREADS, bytes, s>>>(a, pieces, status);
+    kernel<<<(unsigned)(blocks < most ? blocks : most), GRAD_THREADS, bytes, s>>>(a, pieces, run, status);
     return FEDHE_LAUNCHED();
 }
 
