@@ -588,47 +588,89 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
 // ---- operands that TMA cannot take as they are ----
 
 // The values v as the tensor cores take them: bf16 or fp16 as they are, fp32 as three bf16 pieces whose sum is v (each the rounding
-// of what the pieces before it leave; an infinity or a NaN is its own first piece).  Magnitudes where rows are samples of their own.
+// of what the pieces before it leave; an infinity or a NaN is its own first piece).  Magnitudes where rows are samples of their own; those of dy
+// are summed on the way, for the bias.
 struct StageArgs {
-    MatArg in[2];
+    MatArg in[2];            // x, dy
     uint32_t width[2], pitch[2];
     uint16_t *out[2];
     uint32_t rows;
-    bool magnitudes;
+    bool magnitudes, half;   // half: 16-bit values are fp16
+    float *sums;             // null, or [gridDim.y][3][width of dy], of which the first third is written
 };
+// Blocks take 32 packs of 8 columns and a run of rows; a thread stays with its columns.
+constexpr int STAGE_WARPS = 8;
 template <class T>
-__global__ void __launch_bounds__(256) stage_kernel(const StageArgs a) {
-    constexpr int PIECES = sizeof(T) == 4 ? 3 : 1;
-    const int m = blockIdx.y;
-    const uint32_t width = a.width[m], pitch = a.pitch[m], packs = pitch / 8;
-    const size_t plane = (size_t)a.rows * pitch, all = (size_t)a.rows * packs;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (size_t)gridDim.x * 256) {
-        const size_t r = i / packs;
-        const uint32_t c = (uint32_t)(i % packs) * 8;
-        const T *in = static_cast<const T *>(a.in[m].p) + r * a.in[m].stride + c;
-        Pack<uint16_t, 8> o[PIECES];
+__global__ void __launch_bounds__(32 * STAGE_WARPS) stage_kernel(const StageArgs a) {
+    constexpr int PIECES = sizeof(T) == 4 ? 3 : 1, AHEAD = sizeof(T) == 4 ? 2 : 4;
+    __shared__ float met[STAGE_WARPS][8][32];
+    const int m = blockIdx.z;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32, width = a.width[m], pitch = a.pitch[m], c = (blockIdx.x * 32 + lane) * 8;
+    const size_t plane = (size_t)a.rows * pitch;
+    const uint32_t lo = (uint32_t)((uint64_t)a.rows * blockIdx.y / gridDim.y), hi = (uint32_t)((uint64_t)a.rows * (blockIdx.y + 1) / gridDim.y);
+    const T *in = static_cast<const T *>(a.in[m].p) + c;
+    uint16_t *out = a.out[m] + c;
+    const bool wide = reinterpret_cast<uintptr_t>(a.in[m].p) % 16 == 0 && a.in[m].stride % (16 / sizeof(T)) == 0 && c + 8 <= width;
+    const bool summed = m == 1 && a.sums;
+    float sum[8] = {};
+    if (c < pitch)
+        for (uint32_t r0 = lo + warp; r0 < hi; r0 += STAGE_WARPS * AHEAD) {
+            T v[AHEAD][8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
-            T v = c + e < width ? in[e] : T(0);
-            if constexpr (PIECES == 1) {
-                uint16_t b;
-                memcpy(&b, &v, 2);
-                o[0].v[e] = a.magnitudes ? b & 0x7fffu : b;
-            } else {
-                float left = a.magnitudes ? fabsf(v) : v;
+            for (int j = 0; j < AHEAD; j++) {
+                const uint32_t r = r0 + j * STAGE_WARPS;
+                if (r >= hi) break;
+                const T *from = in + r * a.in[m].stride;
+                if (wide) {
 #pragma unroll
-                for (int q = 0; q < 3; q++) {
-                    __nv_bfloat16 b = __float2bfloat16_rn(left);
-                    // what rounds up to infinity is cut instead
-                    if (__hisinf(b) && !isinf(left)) b = __float2bfloat16_rz(left);
-                    o[q].v[e] = __bfloat16_as_ushort(b);
-                    left = isfinite(left) ? left - __bfloat162float(b) : 0.0f;
+                    for (int q = 0; q < (int)sizeof(T) / 2; q++) reinterpret_cast<uint4 *>(v[j])[q] = reinterpret_cast<const uint4 *>(from)[q];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[j][e] = c + e < width ? from[e] : T(0);
                 }
             }
-        }
 #pragma unroll
-        for (int q = 0; q < PIECES; q++) store_pack<uint16_t, 8>(a.out[m] + q * plane + r * pitch + c, o[q]);
-    }
+            for (int j = 0; j < AHEAD; j++) {
+                const uint32_t r = r0 + j * STAGE_WARPS;
+                if (r >= hi) break;
+                Pack<uint16_t, 8> o[PIECES];
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    if constexpr (PIECES == 1) {
+                        o[0].v[e] = a.magnitudes ? v[j][e] & 0x7fffu : v[j][e];
+                    } else {
+                        float left = a.magnitudes ? fabsf(v[j][e]) : v[j][e];
+                        if (summed) sum[e] += left;
+#pragma unroll
+                        for (int q = 0; q < 3; q++) {
+                            __nv_bfloat16 b = __float2bfloat16_rn(left);
+                            // what rounds up to infinity is cut instead
+                            if (__hisinf(b) && !isinf(left)) b = __float2bfloat16_rz(left);
+                            o[q].v[e] = __bfloat16_as_ushort(b);
+                            left = isfinite(left) ? left - __bfloat162float(b) : 0.0f;
+                        }
+                    }
+                }
+                if constexpr (PIECES == 1) {
+                    if (summed) {
+#pragma unroll
+                        for (int e = 0; e < 8; e++)
+                            sum[e] += a.half ? __half2float(__ushort_as_half(o[0].v[e])) : __bfloat162float(__ushort_as_bfloat16(o[0].v[e]));
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < PIECES; q++) store_pack<uint16_t, 8>(out + q * plane + (size_t)r * pitch, o[q]);
+            }
+        }
+    if (!summed) return;
+#pragma unroll
+    for (int e = 0; e < 8; e++) met[warp][e][lane] = sum[e];
+    __syncthreads();
+    const uint32_t l = threadIdx.x / 8, e = threadIdx.x % 8, col = blockIdx.x * 256 + threadIdx.x;
+    float all = 0.0f;
+#pragma unroll
+    for (int w = 0; w < STAGE_WARPS; w++) all += met[w][e][l];
+    if (col < width) a.sums[(size_t)blockIdx.y * 3 * width + col] = all;
 }
 
 inline uint32_t pitch_of(size_t width) { return (uint32_t)((width + 7) / 8 * 8); }
@@ -713,25 +755,34 @@ size_t linear_map_work_bytes(size_t rows, size_t inputs, size_t outputs, int dty
 
 cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *status, cudaStream_t s) {
     uint8_t *work = static_cast<uint8_t *>(a.work);
+    const bool alone = a.over == SumOver::ROWS;
+    float *sums = reinterpret_cast<float *>(work);
     if (a.bias) {
-        const ColumnSumArgs b{a.dy, a.rows, a.outputs, a.over, a.offsets, a.samples, a.accumulate, a.bias, work};
-        const cudaError_t rc = launch_column_sums(b, dtype, n_sm, s);
-        if (rc != cudaSuccess) return rc;
+        if (!alone || !a.rows) {
+            const ColumnSumArgs b{a.dy, a.rows, a.outputs, alone ? SumOver::ALL : a.over, a.offsets, a.samples, a.accumulate, a.bias, work};
+            const cudaError_t rc = launch_column_sums(b, dtype, n_sm, s);
+            if (rc != cudaSuccess) return rc;
+        }
         work += (column_sums_work_bytes(a.rows, a.outputs, n_sm) + 255) / 256 * 256;
     }
     if (!a.rows) return a.accumulate ? cudaSuccess : cudaMemsetAsync(a.weight, 0, a.inputs * a.outputs * sizeof(float), s);
-    const bool alone = a.over == SumOver::ROWS;
     MatArg x = a.x, dy = a.dy;
     uint32_t parts = 1;
     if (alone || !linear_map_aligned(a.x, a.inputs, dtype) || !linear_map_aligned(a.dy, a.outputs, dtype)) {
         uint16_t *to = reinterpret_cast<uint16_t *>(work);
+        const bool summed = alone && a.bias;
         const StageArgs g{{a.x, a.dy}, {(uint32_t)a.inputs, (uint32_t)a.outputs}, {pitch_of(a.inputs), pitch_of(a.outputs)}, {to, to + staged_words(a.rows, a.inputs, dtype)},
-                          (uint32_t)a.rows, alone};
-        const size_t packs = a.rows * (size_t)(g.pitch[0] > g.pitch[1] ? g.pitch[0] : g.pitch[1]) / 8, most = (size_t)16 * n_sm;
-        const dim3 grid((unsigned)((packs + 255) / 256 < most ? (packs + 255) / 256 : most), 2);
-        if (dtype == HE_F32) stage_kernel<float><<<grid, 256, 0, s>>>(g);
-        else stage_kernel<uint16_t><<<grid, 256, 0, s>>>(g);
-        const cudaError_t rc = FEDHE_LAUNCHED();
+                          (uint32_t)a.rows, alone, dtype == HE_F16, summed ? sums : nullptr};
+        const uint32_t columns = (g.pitch[0] > g.pitch[1] ? g.pitch[0] : g.pitch[1]) / 8;
+        // as many runs as column_sums_work_bytes() has room for, at most; four blocks on an SM
+        const size_t cols = (columns + 31) / 32, wanted = ((size_t)2 * n_sm + cols - 1) / cols, rows = (a.rows + STAGE_WARPS - 1) / STAGE_WARPS;
+        size_t runs = wanted < rows ? wanted : rows;
+        if (runs > (size_t)n_sm) runs = n_sm;
+        const dim3 grid((unsigned)cols, (unsigned)runs, 2);
+        if (dtype == HE_F32) stage_kernel<float><<<grid, 32 * STAGE_WARPS, 0, s>>>(g);
+        else stage_kernel<uint16_t><<<grid, 32 * STAGE_WARPS, 0, s>>>(g);
+        cudaError_t rc = FEDHE_LAUNCHED();
+        if (rc == cudaSuccess && summed) rc = launch_join_sums(sums, (uint32_t)runs, a.outputs, a.accumulate, a.bias, s);
         if (rc != cudaSuccess) return rc;
         x = MatArg{g.out[0], g.pitch[0]};
         dy = MatArg{g.out[1], g.pitch[1]};

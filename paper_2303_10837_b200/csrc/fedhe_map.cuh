@@ -167,15 +167,17 @@ struct SampleWalk {
     const int32_t *offsets;
     uint32_t count, k;
     int64_t begin, end;      // of sample k
-    // the first sample that ends behind `row`
+    // the first sample that ends behind `row`; by a whole warp, whose lanes look at 32 places at once
     __device__ __forceinline__ void seek(const int32_t *off, uint32_t n, int64_t row) {
         offsets = off;
         count = n;
         uint32_t lo = 0, hi = n;
         while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if ((int64_t)__ldg(off + mid + 1) > row) hi = mid;
-            else lo = mid + 1;
+            const uint32_t step = (hi - lo + 31) / 32, at = lo + (threadIdx.x & 31u) * step;
+            const uint32_t before = __popc(__ballot_sync(0xffffffffu, at < hi && (int64_t)__ldg(off + min(at, n - 1) + 1) <= row));
+            hi = min(hi, lo + before * step);
+            if (before) lo += (before - 1) * step + 1;
+            else hi = lo;
         }
         k = lo;
         bounds();

@@ -54,7 +54,8 @@ struct NormArgs {
 };
 cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
-// How rows are summed: all of them, or within a sample with the magnitudes added over the samples, or every row a sample of its own.
+// How rows are summed: all of them, or within a sample with the magnitudes added over the samples, or every row a sample of its own (linear
+// layers).
 enum class SumOver { ALL, SAMPLES, ROWS };
 
 struct NormGradArgs {
@@ -73,7 +74,7 @@ struct NormGradArgs {
 size_t norm_grad_work_bytes(size_t rows, size_t width, int n_sm);
 cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, int *status, cudaStream_t s);
 
-// Sums of the columns of a matrix, dst (+)= the sums; work of column_sums_work_bytes()
+// Sums of the columns of a matrix, over all rows or over samples, dst (+)= the sums; work of column_sums_work_bytes()
 struct ColumnSumArgs {
     MatArg m;
     size_t rows, width;
@@ -86,6 +87,8 @@ struct ColumnSumArgs {
 };
 size_t column_sums_work_bytes(size_t rows, size_t width, int n_sm);
 cudaError_t launch_column_sums(const ColumnSumArgs &a, int dtype, int n_sm, cudaStream_t s);
+// dst (+)= the sum of `runs` partial sums of columns, the first `width` of 3 * width words of each
+cudaError_t launch_join_sums(const float *heads, uint32_t runs, size_t width, bool accumulate, float *dst, cudaStream_t s);
 
 struct LinearMapArgs {
     MatArg x, dy;

@@ -145,7 +145,7 @@ struct RowPlan {
     uint32_t threads, groups, depth;
     uint32_t room;                                           // bytes of a row in shared memory
 };
-constexpr uint32_t MOST_DEPTH = 8;
+constexpr uint32_t MOST_DEPTH = 4;
 // false: the row is too long for one block
 inline bool plan_row(size_t width, size_t element, uint32_t block, uint32_t held, uint32_t rows_at_once, size_t ring, RowPlan &p) {
     const size_t t = (width + held - 1) / held;
@@ -552,7 +552,7 @@ template <class T, int V, bool X>
 __global__ void __launch_bounds__(SUM_COLS * SUM_WARPS) sums_kernel(const MatArg m, const MatArg xm, const float *mean, const float *rstd, const size_t rows,
                                                                     const size_t width, const SumOver over, const int32_t *offsets,
                                                                     const uint32_t samples, const RunsOut out) {
-    constexpr int P = X ? 2 : 1, AHEAD = 4;
+    constexpr int P = X ? 2 : 1, AHEAD = X ? 4 : 8;
     __shared__ float runs[3][SUM_WARPS][V][SUM_COLS];
     __shared__ int cuts[SUM_WARPS];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32, run = blockIdx.y;
@@ -564,22 +564,25 @@ __global__ void __launch_bounds__(SUM_COLS * SUM_WARPS) sums_kernel(const MatArg
     for (int p = 0; p < P; p++)
 #pragma unroll
         for (int e = 0; e < V; e++) sum[p][e] = head[p][e] = inner[p][e] = 0.0f;
-    int cut = over == SumOver::ROWS;         // magnitudes of rows: all of them are inner
+    int cut = 0;
     SampleWalk walk;
     walk.begin = 0;
     walk.end = INT64_MAX;
-    if (over == SumOver::SAMPLES) {
-        walk.seek(offsets, samples, (int64_t)begin);
-        cut = walk.begin == (int64_t)begin;  // the run before this one ends with another sample
-    }
-    for (size_t r0 = begin; r0 < end; r0 += AHEAD) {
-        Pack<T, V> g[AHEAD], x[X ? AHEAD : 1];
+    Pack<T, V> g[AHEAD], x[X ? AHEAD : 1];
+    const auto load = [&](size_t r0) {
 #pragma unroll
         for (int j = 0; j < AHEAD; j++)
             if (r0 + j < end && col < width) {
                 g[j] = load_pack<T, V>(static_cast<const T *>(m.p) + (r0 + j) * m.stride + col);
                 if (X) x[X ? j : 0] = load_pack<T, V>(static_cast<const T *>(xm.p) + (r0 + j) * xm.stride + col);
             }
+    };
+    load(begin);
+    if (over == SumOver::SAMPLES) {
+        walk.seek(offsets, samples, (int64_t)begin);
+        cut = walk.begin == (int64_t)begin;  // the run before this one ends with another sample
+    }
+    for (size_t r0 = begin; r0 < end;) {
 #pragma unroll
         for (int j = 0; j < AHEAD; j++) {
             const size_t r = r0 + j;
@@ -597,19 +600,16 @@ __global__ void __launch_bounds__(SUM_COLS * SUM_WARPS) sums_kernel(const MatArg
                 walk.next((int64_t)r);
             }
             if ((int64_t)r < walk.begin || col >= width) continue;      // no sample's row
-            if (over == SumOver::ROWS) {
+            if (X) {
+                const float mu = mean[r], rs = rstd[r];
 #pragma unroll
-                for (int e = 0; e < V; e++) inner[P - 1][e] += fabsf(to_f32(g[j].v[e]));
-            } else {
-                if (X) {
-                    const float mu = mean[r], rs = rstd[r];
-#pragma unroll
-                    for (int e = 0; e < V; e++) sum[0][e] = fmaf(to_f32(g[j].v[e]), (to_f32(x[X ? j : 0].v[e]) - mu) * rs, sum[0][e]);
-                }
-#pragma unroll
-                for (int e = 0; e < V; e++) sum[P - 1][e] += to_f32(g[j].v[e]);
+                for (int e = 0; e < V; e++) sum[0][e] = fmaf(to_f32(g[j].v[e]), (to_f32(x[X ? j : 0].v[e]) - mu) * rs, sum[0][e]);
             }
+#pragma unroll
+            for (int e = 0; e < V; e++) sum[P - 1][e] += to_f32(g[j].v[e]);
         }
+        r0 += AHEAD;
+        if (r0 < end) load(r0);
     }
     if (lane == 0) cuts[warp] = cut;
 #pragma unroll
@@ -649,11 +649,12 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) sums_join_kernel(const RunsOu
     float *dst = plane ? dst1 : dst0;
     Run all{0.0f, 0.0f, 0.0f, 0};
     const uint32_t begin = in.runs * warp / JOIN_WARPS, end = in.runs * (warp + 1) / JOIN_WARPS;
+    constexpr int AHEAD = 5;                 // of 148 runs a warp has five at most
     if (col < in.width)
-        for (uint32_t r0 = begin; r0 < end; r0 += 4) {
-            Run part[4];
+        for (uint32_t r0 = begin; r0 < end; r0 += AHEAD) {
+            Run part[AHEAD];
 #pragma unroll
-            for (int j = 0; j < 4; j++) {
+            for (int j = 0; j < AHEAD; j++) {
                 part[j] = Run{0.0f, 0.0f, 0.0f, 0};
                 if (r0 + j >= end) continue;
                 part[j].head = in.of(r0 + j, 0, plane)[col];
@@ -664,13 +665,17 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) sums_join_kernel(const RunsOu
                 }
             }
 #pragma unroll
-            for (int j = 0; j < 4; j++) all.join(part[j]);
+            for (int j = 0; j < AHEAD; j++) all.join(part[j]);
         }
     runs[warp][lane] = all;
-    __syncthreads();
+    for (uint32_t step = 1; step < JOIN_WARPS; step *= 2) {
+        __syncthreads();
+        if (warp % (2 * step) == 0) {
+            all.join(runs[warp + step][lane]);
+            runs[warp][lane] = all;
+        }
+    }
     if (warp || col >= in.width) return;
-#pragma unroll 4
-    for (int w = 1; w < JOIN_WARPS; w++) all.join(runs[w][lane]);
     const float v = MAGNITUDES ? fabsf(all.head) + all.inner + fabsf(all.tail) : all.head;
     dst[col] = accumulate ? dst[col] + v : v;
 }
@@ -782,6 +787,11 @@ cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, int *status, cud
     return dtype == HE_F32    ? norm_of<float>(a, n_sm, status, s)
            : dtype == HE_BF16 ? norm_of<__nv_bfloat16>(a, n_sm, status, s)
                               : norm_of<__half>(a, n_sm, status, s);
+}
+
+// The runs' heads, summed.
+cudaError_t launch_join_sums(const float *heads, uint32_t runs, size_t width, bool accumulate, float *dst, cudaStream_t s) {
+    return join_runs(RunsOut{const_cast<float *>(heads), runs, width, 1}, false, accumulate, dst, nullptr, s);
 }
 
 size_t norm_grad_work_bytes(size_t rows, size_t width, int n_sm) { return runs_bytes(rows, width, 2, n_sm); }
