@@ -21,8 +21,13 @@ constexpr uint32_t DEPTH = 128;
 constexpr uint32_t GROUP = 64;                          // columns of a swizzled group: 128 bytes of each row
 constexpr uint32_t SLOTS = 16;                          // stages under way, at most
 constexpr uint32_t RING_BYTES = 196608;
-// Boxes of a copy have 128, 64, 32 or 16 rows: a stage is copied in as many as its rows have bits, no further than the next sixteen.
+// Boxes of a copy have 128, 64, 32 or 16 rows.  A stage's rows are rounded up to sixteens, and three or seven of those to four or eight, which one
+// box brings; then they are copied in as many boxes as their number has bits.
 constexpr int BOXES = 4;
+__device__ __forceinline__ uint32_t padded(uint32_t rows) {
+    const uint32_t n = (rows + 15) / 16;
+    return (n % 4 == 3 ? n + 1 : n) * 16;
+}
 struct Maps {
     CUtensorMap dy[BOXES], x[BOXES];
 };
@@ -353,12 +358,12 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                     const uint32_t left = e.what & Stage::ROWS, pair = e.what >> Stage::PAIR, slot = stage % SLOTS, ends = left & 15u;
                     const int32_t plane = job.pairs == 1 ? 0 : (int32_t)(of_dy ? piece_of_dy(pair) : piece_of_x(pair));
                     const int32_t row = e.row;
-                    const uint32_t rows = (left + 15) & ~15u;
+                    const uint32_t rows = padded(left);
                     e = list[i + 1];
                     while (well && (room < rows || i - oldest >= SLOTS)) {
                         const uint32_t was = stage - (i - oldest);
                         well = bar_wait(&empty[was % SLOTS], was / SLOTS & 1u);
-                        room += ((list[oldest].what & Stage::ROWS) + 15) & ~15u;
+                        room += padded(list[oldest].what & Stage::ROWS);
                         oldest++;
                     }
                     if (!well) break;
@@ -420,7 +425,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                             if (what & Stage::ENDS) commit<CG>(&sum_full[b], (uint16_t)(3u << leader));
                         }
                         __syncwarp();
-                        at += sixteens * 16;
+                        at += padded(what & Stage::ROWS);
                         if (at >= job.ring) at -= job.ring;
                     }
             } else {
@@ -433,7 +438,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         if (over) {
                             well = bar_wait(&part[slot], parts >> slot & 1u);
                             if (!well) break;
-                            uint32_t from = at + left - over;    // the last sixteen rows: the ring's end is a multiple of 16
+                            uint32_t from = at + left - over;    // the sample's last sixteen rows: the ring's end is a multiple of 16
                             if (from >= job.ring) from -= job.ring;
                             for (uint32_t g = lane / 8; g < 2 + nb / GROUP; g += 4) {
                                 const uint32_t to = smem + g * pitch_group + from * 128 + lane % 8 * 16;
@@ -451,7 +456,7 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                         __syncwarp();
                     }
                     if (over) parts ^= 1u << slot;
-                    at += (left + 15) & ~15u;
+                    at += padded(left);
                     if (at >= job.ring) at -= job.ring;
                 }
             }

@@ -703,9 +703,10 @@ template <class T, bool X>
 cudaError_t sums(const MatArg &m, const MatArg &x, const float *mean, const float *rstd, size_t rows, size_t width, SumOver over,
                  const int32_t *offsets, uint32_t samples, bool accumulate, float *dst0, float *dst1, void *work, int n_sm, cudaStream_t s) {
     const bool wide = wide_rows<T>(m.p, m.stride, width) && (!X || wide_rows<T>(x.p, x.stride, width));
-    const RunsOut out{static_cast<float *>(work), sum_runs(rows, n_sm), width, X ? 2 : 1};
-    const unsigned cols = SUM_COLS * (wide ? WIDE<T> : 1);
-    const dim3 grid(blocks_for(width, cols), out.runs);
+    // two blocks on an SM
+    const unsigned cols = blocks_for(width, SUM_COLS * (wide ? WIDE<T> : 1)), most = (2 * n_sm + cols - 1) / cols, runs = sum_runs(rows, n_sm);
+    const RunsOut out{static_cast<float *>(work), runs < most ? runs : most, width, X ? 2 : 1};
+    const dim3 grid(cols, out.runs);
     if (wide) sums_kernel<T, WIDE<T>, X><<<grid, SUM_COLS * SUM_WARPS, 0, s>>>(m, x, mean, rstd, rows, width, over, offsets, samples, out);
     else sums_kernel<T, 1, X><<<grid, SUM_COLS * SUM_WARPS, 0, s>>>(m, x, mean, rstd, rows, width, over, offsets, samples, out);
     const cudaError_t rc = FEDHE_LAUNCHED();
