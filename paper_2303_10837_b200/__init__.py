@@ -574,33 +574,36 @@ def _dtype(t: torch.Tensor, what: str) -> int:
 
 def _matrix(t: torch.Tensor, rows: Optional[int], cols: Optional[int], dtype: Optional[torch.dtype], what: str, out: bool = False) -> int:
     """Row stride of a matrix whose rows are contiguous; its sizes and type are checked (None: any)."""
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise HeError(HE_ERR_INVALID_ARG, "%s: shape %s, [%s][%s] needed" % (what, tuple(t.shape), "rows" if rows is None else rows,
+    shape = t.shape
+    if len(shape) != 2 or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+        raise HeError(HE_ERR_INVALID_ARG, "%s: shape %s, [%s][%s] needed" % (what, tuple(shape), "rows" if rows is None else rows,
                                                                              "columns" if cols is None else cols))
     if dtype is not None and t.dtype != dtype:
         raise HeError(HE_ERR_INVALID_ARG, "%s: %s, %s needed" % (what, t.dtype, dtype))
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    stride, step = t.stride()
+    if step != 1 and shape[1] > 1:
         raise HeError(HE_ERR_INVALID_ARG, "%s: the elements of a row do not lie together" % what)
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
-    if out and stride < t.shape[1]:
+    if shape[0] < 2:
+        stride = shape[1]
+    if out and stride < shape[1]:
         raise HeError(HE_ERR_INVALID_ARG, "%s: rows overlap" % what)
     return stride
 
 
-def _vector(t: torch.Tensor, count: int, dtype, what: str) -> None:
-    if t.dim() != 1 or t.shape[0] != count or t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)) or (count > 1 and t.stride(0) != 1):
+def _vector(t: torch.Tensor, count: int, dtype: torch.dtype, what: str, dtype2: Optional[torch.dtype] = None) -> None:
+    if len(t.shape) != 1 or t.shape[0] != count or (t.dtype != dtype and t.dtype != dtype2) or (count > 1 and t.stride(0) != 1):
         raise HeError(HE_ERR_INVALID_ARG, "%s: %s %s, a contiguous vector of %d needed" % (what, t.dtype, tuple(t.shape), count))
 
 
-def _on_gpu(first: torch.Tensor, *more: Optional[torch.Tensor]) -> int:
+def _on_gpu(*tensors: Optional[torch.Tensor]) -> int:
     """All tensors lie on the current device (None: absent)."""
-    device = torch.cuda.current_device() if first.is_cuda else -1
-    for t in (first,) + more:
-        if t is not None:
-            if not t.is_cuda:
-                raise TypeError("expected CUDA tensors")
-            if t.get_device() != device:
-                raise HeError(HE_ERR_INVALID_ARG, "a tensor on cuda:%d, the current device is cuda:%d" % (t.get_device(), device))
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            raise TypeError("expected CUDA tensors")
+    device = _raw_device() if _raw_device else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise HeError(HE_ERR_INVALID_ARG, "a tensor on cuda:%d, the current device is cuda:%d" % (t.get_device(), device))
     return device
 
 
@@ -677,13 +680,15 @@ def he_token_log_probs_backward(ctx: Ctx, logits: torch.Tensor, targets: torch.T
 
 def _norm_weights(weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], width: int, x: torch.Tensor, what: str) -> int:
     """Type of the weights: float32 or x's, both the same."""
-    kinds = [t.dtype for t in (weight, bias) if t is not None]
-    for t in (weight, bias):
-        if t is not None:
-            _vector(t, width, (torch.float32, x.dtype), what + "weights")
-    if len(kinds) == 2 and kinds[0] != kinds[1]:
-        raise HeError(HE_ERR_INVALID_ARG, what + "weight and bias: %s and %s" % (kinds[0], kinds[1]))
-    return _DTYPES[kinds[0]] if kinds else HE_F32
+    first = weight if weight is not None else bias
+    if first is None:
+        return HE_F32
+    _vector(first, width, torch.float32, what + "weights", x.dtype)
+    if bias is not None and bias is not first:
+        _vector(bias, width, torch.float32, what + "bias", x.dtype)
+        if bias.dtype != first.dtype:
+            raise HeError(HE_ERR_INVALID_ARG, what + "weight and bias: %s and %s" % (first.dtype, bias.dtype))
+    return _DTYPES[first.dtype]
 
 
 def he_layer_norm(ctx: Ctx, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,

@@ -435,7 +435,10 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                     const uint32_t left = e.what & Stage::ROWS, slot = stage % SLOTS, over = left & 15u;
                     e = list[i + 1];
                     if (stage % (EPILOGUE - CHECKS) == warp - CHECKS) {
-                        if (over) {
+                        // The slot's last stage is done with, and with it the last phase of `part`: a warp that asks for the phase after one that
+                        // is not over is told that it is.
+                        if (stage >= SLOTS) well = bar_wait(&empty[slot], stage / SLOTS & 1u ^ 1u);
+                        if (well && over) {
                             well = bar_wait(&part[slot], parts >> slot & 1u);
                             if (!well) break;
                             uint32_t from = at + left - over;    // the sample's last sixteen rows: the ring's end is a multiple of 16
@@ -448,9 +451,6 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
                             }
                             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                             __syncwarp();
-                        } else if (stage >= SLOTS) {
-                            // the slot's last stage is done with
-                            well = bar_wait(&empty[slot], stage / SLOTS & 1u ^ 1u);
                         }
                         if (well && elected()) bar_arrive(&full[slot], leader);
                         __syncwarp();
@@ -730,7 +730,7 @@ Plan plan_of(const LinearMapArgs &a, uint32_t pairs, int n_sm) {
 template <int CG>
 cudaError_t launch(const Maps &maps, const LinearJob &job, uint32_t tiles, cudaStream_t s) {
     const uint32_t bytes = (RING_BYTES > STAGING ? RING_BYTES : STAGING) + 1024;
-    cudaError_t rc = cudaFuncSetAttribute(linear_map_kernel<CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t rc = allow_shared(reinterpret_cast<const void *>(linear_map_kernel<CG>), bytes);
     if (rc != cudaSuccess) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(tiles * job.splits * CG);

@@ -10,6 +10,29 @@
 
 namespace fedhe {
 
+// Dynamic shared memory of a block, at most: all that there is less what the kernels hold besides (11 KB) and the system's 1 KB.
+constexpr size_t MOST_SHARED = 216 << 10;
+// A kernel's shared memory beyond 48 KB has to be allowed, for each device: asked for once by each host thread, and for the most that any call needs,
+// so that no other thread's call lowers it.
+inline cudaError_t allow_shared(const void *kernel, size_t bytes) {
+    struct Allowed {
+        const void *kernel;
+        int device;
+    };
+    constexpr int PLACES = 64;
+    thread_local Allowed known[PLACES] = {};
+    int device = 0;
+    if (bytes <= 32 << 10) return cudaSuccess;
+    if (bytes > MOST_SHARED) return cudaErrorInvalidValue;
+    const cudaError_t rc = cudaGetDevice(&device);
+    if (rc != cudaSuccess) return rc;
+    Allowed &a = known[(reinterpret_cast<uintptr_t>(kernel) / 16 + device * 7) % PLACES];
+    if (a.kernel == kernel && a.device == device) return cudaSuccess;
+    const cudaError_t set = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_SHARED);
+    if (set == cudaSuccess) a = Allowed{kernel, device};
+    return set;
+}
+
 template <class T>
 __device__ __forceinline__ float to_f32(T v);
 template <>

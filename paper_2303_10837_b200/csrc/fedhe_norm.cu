@@ -715,16 +715,13 @@ cudaError_t sums(const MatArg &m, const MatArg &x, const float *mean, const floa
 
 inline uint32_t row_threads(size_t packs) { return packs >= 256 ? 256 : (uint32_t)(packs + 31) / 32 * 32; }
 
-// Shared memory of a block: all that there is less what the kernels hold besides, for as many blocks as share an SM.
-constexpr size_t SHARED = 220 << 10;
-
 template <class T, int V, int HELD, int THREADS, int BLOCKS>
 bool norm_go(const NormArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
     RowPlan plan;
-    if (!plan_row(a.width, sizeof(T), THREADS, HELD, 1, SHARED / BLOCKS - 4096, plan)) return false;
+    if (!plan_row(a.width, sizeof(T), THREADS, HELD, 1, MOST_SHARED / BLOCKS - 1024, plan)) return false;
     const auto kernel = norm_kernel<T, V, HELD, THREADS, BLOCKS>;
     const size_t bytes = (size_t)plan.groups * plan.depth * plan.room, blocks = (a.rows + plan.groups - 1) / plan.groups, most = (size_t)BLOCKS * n_sm;
-    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    rc = allow_shared(reinterpret_cast<const void *>(kernel), bytes);
     if (rc != cudaSuccess) return true;
     kernel<<<(unsigned)(blocks < most ? blocks : most), THREADS, bytes, s>>>(a, plan, status);
     rc = FEDHE_LAUNCHED();
@@ -749,11 +746,11 @@ bool norm_grad_go(const NormGradArgs &a, uint32_t depth, int n_sm, int *status, 
     const size_t t = ((a.width + HELD - 1) / HELD + 31) / 32 * 32;
     if (t > BACK_THREADS) return false;
     const size_t plane = (BACK_THREADS / t) * 2 * a.width * sizeof(float), kept = SAMPLES ? (2 * plane + 15) / 16 * 16 : 0;
-    if (kept > SHARED - 4096 || !plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, SHARED - 4096 - kept, plan) || plan.depth < depth) return false;
+    if (kept > MOST_SHARED || !plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, MOST_SHARED - kept, plan) || plan.depth < depth) return false;
     const auto kernel = norm_grad_kernel<T, V, HELD, SAMPLES>;
     const size_t copies = (size_t)plan.groups * plan.depth * 2 * plan.room, bytes = kept + (copies > plane ? copies : plane);
     const RunsOut out{static_cast<float *>(a.work), sum_runs(a.rows, n_sm), a.width, 2};
-    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    rc = allow_shared(reinterpret_cast<const void *>(kernel), bytes);
     if (rc != cudaSuccess) return true;
     kernel<<<out.runs, BACK_THREADS, bytes, s>>>(a, plan, out, status);
     rc = FEDHE_LAUNCHED();

@@ -430,7 +430,7 @@ cudaError_t log_probs_of(const LogProbsArgs &a, int n_sm, int *status, cudaStrea
     while (C < 8 && 2 * C <= pieces && a.rows * 2 * C <= most + n_sm) C *= 2;
     const size_t clusters = most / C ? most / C : 1;
     const auto kernel = a.top ? log_probs_kernel<T, true> : log_probs_kernel<T, false>;
-    cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    cudaError_t rc = allow_shared(reinterpret_cast<const void *>(kernel), bytes);
     if (rc != cudaSuccess) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(nt);
@@ -629,7 +629,7 @@ cudaError_t log_probs_grad_of(const LogProbsGradArgs &a, int n_sm, int *status, 
     const auto kernel = a.top           ? (a.dentropy ? log_probs_grad_kernel<T, true, true> : log_probs_grad_kernel<T, false, true>)
                         : a.dentropy    ? log_probs_grad_kernel<T, true, false>
                                         : log_probs_grad_kernel<T, false, false>;
-    const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    const cudaError_t rc = allow_shared(reinterpret_cast<const void *>(kernel), bytes);
     if (rc != cudaSuccess) return rc;
     kernel<<<(unsigned)(blocks < most ? blocks : most), GRAD_THREADS, bytes, s>>>(a, pieces, run, stream, status);
     return FEDHE_LAUNCHED();

@@ -328,6 +328,29 @@ def test_linear_sensitivity_of_a_long_sample(ctx):
         assert float((gw.double() - w).norm() / w.norm()) < 2e-6
 
 
+@pytest.mark.parametrize("inputs,outputs", [(512, 512), (4096, 1024), (640, 2000), (2048, 129)])
+@pytest.mark.parametrize("lengths", [[300, 600, 64, 520, 600], [17, 128, 300, 520, 64, 33, 600, 1, 16, 15], [1, 2, 3, 16, 17], [128], [2000, 5, 700]])
+def test_linear_sensitivity_of_many_samples_is_exact_in_whole_numbers(ctx, inputs, outputs, lengths):
+    """Sums of whole numbers below 2^24 have no rounding: every order of the work gives the same, whatever waits for what inside the kernel."""
+    import random
+    rng = random.Random(len(lengths) + inputs)
+    lens = [rng.choice(lengths) for _ in range(min(60, 20000 // max(lengths) + 8))]
+    g = gen(inputs)
+    x = torch.randint(-2, 3, (sum(lens), inputs), generator=g, device="cuda").bfloat16()
+    dy = torch.randint(-2, 3, (sum(lens), outputs), generator=g, device="cuda").bfloat16()
+    cuts = [0]
+    for n in lens:
+        cuts.append(cuts[-1] + n)
+    want = torch.zeros(outputs, inputs, device="cuda")
+    for lo, hi in zip(cuts, cuts[1:]):
+        want += (dy[lo:hi].float().T @ x[lo:hi].float()).abs()
+    for _ in range(4):
+        assert torch.equal(he.he_linear_sensitivity(ctx, x, dy, samples=offsets(cuts))[0], want)
+    alone = (dy.float().abs().T @ x.float().abs())
+    assert torch.equal(he.he_linear_sensitivity(ctx, x, dy)[0], alone)
+    assert he.he_ctx_status(ctx) == 0
+
+
 def test_linear_sensitivity_of_no_rows(ctx):
     x, dy = torch.empty(0, 8, device="cuda"), torch.empty(0, 5, device="cuda")
     for samples in (None, offsets([0]), offsets([0, 0, 0])):

@@ -119,7 +119,7 @@ def test_a_tensor_on_another_device_is_refused(monkeypatch):
         def get_device(self):
             return self.device
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(he, "_raw_device", lambda: 1)
     assert he._on_gpu(Far(1), None, Far(1)) == 1
     for tensors in ((Far(0),), (Far(1), None, Far(0))):
         refused(lambda: he._on_gpu(*tensors))
