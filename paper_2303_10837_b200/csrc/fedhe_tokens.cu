@@ -15,7 +15,7 @@ namespace fedhe {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float FAR = -1e30f;             // exponents stop here: 2^FAR is 0, and FAR times 0 is 0, not NaN
+constexpr float FAR = -1e20f;             // exponents stop here: 2^FAR is 0, and FAR times what a row sums up to or a gradient is no infinity
 constexpr int PACKS = 4;                  // of 16 bytes, that a thread has of a piece
 constexpr uint32_t FOUND = 512;           // candidates that a block can hold
 constexpr uint32_t DEPTH = 3;             // pieces that a warp asks for ahead
@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, GRAD_BLOCKS) log_probs_grad_kern
                     }
                 }
             }
-    }
+        }
         r = r_next;
         part = part_next;
     }
