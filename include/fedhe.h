@@ -367,7 +367,7 @@ int he_round_host(he_ctx *ctx, const he_keys *keys, const he_mask *mask, const f
  *     ascending or reach beyond the rows give unspecified sums, never an access
  *     out of bounds.
  *   - Statistics, sums and map entries are fp32 whatever the dtype.  Results
- *     do not depend on timing: the same call gives the same bits.
+ *     do not depend on timing: the same call gives the same bits on a GPU.
  *   - Nothing is allocated: scratch comes from the caller (work, 16-byte
  *     aligned, of at least the bytes that *_work_bytes names), so calls that
  *     have scratch of their own may overlap on any streams, and all of

@@ -706,22 +706,66 @@ bool tensor_map(CUtensorMap &m, const void *p, size_t width, size_t rows, size_t
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a product is shared out.
+constexpr uint32_t SHARED = (RING_BYTES > STAGING ? RING_BYTES : STAGING) + 1024;
+constexpr uint32_t MOST_CLUSTER = 8;
+
+cudaError_t configure(cudaLaunchConfig_t &cfg, cudaLaunchAttribute &at, const void *kernel, uint32_t blocks, uint32_t cluster, cudaStream_t s) {
+    cfg.gridDim = dim3(blocks);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SHARED;
+    cfg.stream = s;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim = {cluster, 1, 1};
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return allow_shared(kernel, SHARED);
+}
+
+// Clusters of 1 to MOST_CLUSTER blocks that the GPU runs at once.  A cluster stays in a part of the GPU whose SMs it need not fill: of 148 SMs
+// clusters of four have 132, of seven 105.  Asked for once by each host thread and device.
+struct Clusters {
+    int device = -1;
+    int count[MOST_CLUSTER + 1];
+};
+cudaError_t clusters_at_once(const Clusters *&got) {
+    thread_local Clusters known;
+    int device = 0;
+    cudaError_t rc = cudaGetDevice(&device);
+    if (rc != cudaSuccess) return rc;
+    got = &known;
+    if (known.device == device) return cudaSuccess;
+    for (uint32_t c = 1; c <= MOST_CLUSTER; c++) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at;
+        rc = configure(cfg, at, reinterpret_cast<const void *>(linear_map_kernel<1>), c, c, nullptr);
+        if (rc == cudaSuccess) rc = cudaOccupancyMaxActiveClusters(&known.count[c], linear_map_kernel<1>, &cfg);
+        if (rc != cudaSuccess) return rc;
+    }
+    known.device = device;
+    return cudaSuccess;
+}
+
+// How a product is shared out: the blocks of a tile, its inputs, and how many share its samples.  The least of an estimate in clocks, fitted to the
+// times of all choices at 17 shapes of 64 to 16384 rows and 128 to 8192 columns, where it is 0.8 % above the best on the mean (with as many clusters at
+// once as SMs would hold, 40 %: 16384 x 640 x 640 in 512 samples takes 68 us in tiles of 256 shared by eight, 129 shared by seven).  Pairs read x half
+// as often: 131 us for 16384 x 2048 x 2048 in 64 samples, 176 by single blocks; small maps have too few tiles for them.
 struct Plan {
     uint32_t cg, n, splits;
 };
-Plan plan_of(const LinearMapArgs &a, uint32_t pairs, int n_sm) {
+Plan plan_of(const LinearMapArgs &a, uint32_t pairs, const Clusters &clusters) {
     Plan best{1, 64, 1};
     double least = 1e300;
+    const size_t pieces = a.over == SumOver::SAMPLES ? (size_t)a.samples : (a.rows + PIECE_ALONE - 1) / PIECE_ALONE;
     for (uint32_t cg = 1; cg <= 2; cg++)
         for (uint32_t n = 64 * cg; n <= MOST_N; n += 64 * cg)
-            for (uint32_t c = 1; c * cg <= 8; c++) {
-                if (c > 1 && c > (a.over == SumOver::SAMPLES ? (size_t)a.samples : (a.rows + PIECE_ALONE - 1) / PIECE_ALONE)) break;
+            for (uint32_t c = 1; c * cg <= MOST_CLUSTER; c++) {
+                if (c > 1 && c > pieces) break;
+                if (clusters.count[c * cg] < 1) continue;
                 const double tiles = (double)((a.outputs + 128 * cg - 1) / (128 * cg)) * (double)((a.inputs + n - 1) / n);
-                const double waves = ceil(tiles * cg * c / n_sm);
-                // clocks of a row: its products, or its bytes at what L2 gives an SM
-                const double row = fmax(n / 32.0, (128.0 + n / cg) * 2 / 48);
-                const double t = waves * ((double)a.rows / c * pairs * row + 4000 + 8.0 * n + (c > 1 ? 1500 : 0));
+                const double waves = ceil(tiles / clusters.count[c * cg]);
+                // of a row: its products, or its bytes from L2; of a sample: its way through the epilogue; of a block: its beginning and end
+                const double row = fmax(n / 32.0, (128.0 + n / cg) * 2 / 32), sample = 300 + 2.0 * n, block = 4000 + 8.0 * n + (c > 1 ? 1500 : 0);
+                const double t = waves * ((double)a.rows / c * pairs * row + ceil((double)pieces / c) * sample + block);
                 if (t < least) least = t, best = Plan{cg, n, c};
             }
     return best;
@@ -729,19 +773,10 @@ Plan plan_of(const LinearMapArgs &a, uint32_t pairs, int n_sm) {
 
 template <int CG>
 cudaError_t launch(const Maps &maps, const LinearJob &job, uint32_t tiles, cudaStream_t s) {
-    const uint32_t bytes = (RING_BYTES > STAGING ? RING_BYTES : STAGING) + 1024;
-    cudaError_t rc = allow_shared(reinterpret_cast<const void *>(linear_map_kernel<CG>), bytes);
-    if (rc != cudaSuccess) return rc;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(tiles * job.splits * CG);
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = bytes;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {job.splits * CG, 1, 1};
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cudaLaunchAttribute at;
+    cudaError_t rc = configure(cfg, at, reinterpret_cast<const void *>(linear_map_kernel<CG>), tiles * job.splits * CG, job.splits * CG, s);
+    if (rc != cudaSuccess) return rc;
     rc = cudaLaunchKernelEx(&cfg, linear_map_kernel<CG>, maps, job);
     return rc != cudaSuccess ? rc : FEDHE_LAUNCHED();
 }
@@ -794,7 +829,10 @@ cudaError_t launch_linear_map(const LinearMapArgs &a, int dtype, int n_sm, int *
         parts = dtype == HE_F32 ? 3 : 1;
     }
     const uint32_t pairs = parts == 3 ? 6 : 1;
-    const Plan plan = plan_of(a, pairs, n_sm);
+    const Clusters *clusters;
+    const cudaError_t asked = clusters_at_once(clusters);
+    if (asked != cudaSuccess) return asked;
+    const Plan plan = plan_of(a, pairs, *clusters);
     Maps maps;
     const bool half = dtype == HE_F16;
     for (int i = 0; i < BOXES; i++)
