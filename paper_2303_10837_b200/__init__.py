@@ -630,10 +630,9 @@ def he_token_log_probs(ctx: Ctx, logits: torch.Tensor, targets: torch.Tensor, to
     if vocab < 1 or not 0 <= top <= min(vocab, HE_MAX_TOP):
         raise HeError(HE_ERR_INVALID_ARG, what + "top: %d of %d" % (top, vocab))
     _on_gpu(logits, targets)
-    out = torch.empty((3, rows), dtype=torch.float32, device=logits.device)
-    logp, lse, entropy = out.unbind(0)
-    top_logp = torch.empty((rows, top), dtype=torch.float32, device=logits.device) if top else None
-    top_ids = torch.empty((rows, top), dtype=torch.int64, device=logits.device) if top else None
+    logp, lse, entropy = logits.new_empty((3, rows), dtype=torch.float32).unbind(0)
+    top_logp = logits.new_empty((rows, top), dtype=torch.float32) if top else None
+    top_ids = logits.new_empty((rows, top), dtype=torch.int64) if top else None
     _check(_lib.he_token_log_probs(ctx.handle, _ptr(logits), code, rows, vocab, stride, _ptr(targets), top, _ptr(logp), _ptr(lse),
                                    _ptr(entropy), _ptr(top_logp), _ptr(top_ids), _stream()), "he_token_log_probs")
     return logp, lse, entropy, top_logp, top_ids
@@ -670,7 +669,7 @@ def he_token_log_probs_backward(ctx: Ctx, logits: torch.Tensor, targets: torch.T
         _matrix(out, rows, vocab, logits.dtype, what + "out", out=True)
     _on_gpu(logits, targets, lse, dlogp, entropy, dentropy, top_ids, dtop, out)
     if out is None:
-        out = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
+        out = logits.new_empty((rows, vocab))
     _check(_lib.he_token_log_probs_backward(ctx.handle, _ptr(logits), code, rows, vocab, stride, _ptr(targets), _ptr(lse), _ptr(dlogp),
                                             _ptr(entropy) if dentropy is not None else None, _ptr(dentropy), top, _ptr(top_ids) if top else None,
                                             _ptr(dtop) if top else None, _ptr(out), out.stride(0) if rows > 1 else vocab, _stream()),
@@ -704,8 +703,8 @@ def he_layer_norm(ctx: Ctx, x: torch.Tensor, weight: Optional[torch.Tensor] = No
         _matrix(out, rows, width, x.dtype, what + "out", out=True)
     _on_gpu(x, weight, bias, out)
     if out is None:
-        out = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+        out = x.new_empty((rows, width))
+    mean, rstd = x.new_empty((2, rows), dtype=torch.float32).unbind(0)
     _check(_lib.he_layer_norm(ctx.handle, _ptr(x), code, rows, width, stride, _ptr(weight), _ptr(bias), kind, eps, _ptr(out),
                               out.stride(0) if rows > 1 else width, _ptr(mean), _ptr(rstd), _stream()), "he_layer_norm")
     return out, mean, rstd
@@ -726,12 +725,12 @@ def he_layer_norm_backward(ctx: Ctx, dy: torch.Tensor, x: torch.Tensor, mean: to
     if width < 1:
         raise HeError(HE_ERR_INVALID_ARG, what + "x: no columns")
     _on_gpu(x, dy, mean, rstd, weight, samples)
-    dx = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-    dweight, dbias = torch.empty((2, width), dtype=torch.float32, device=x.device).unbind(0)
-    room = _lib.he_layer_norm_backward_work_bytes(ctx.handle, rows, width)
-    work = torch.empty(max(room, 16), dtype=torch.uint8, device=x.device)
+    dx = x.new_empty((rows, width))
+    dweight, dbias = x.new_empty((2, width), dtype=torch.float32).unbind(0)
+    room = max(_lib.he_layer_norm_backward_work_bytes(ctx.handle, rows, width), 16)
+    work = x.new_empty(room, dtype=torch.uint8)
     _check(_lib.he_layer_norm_backward(ctx.handle, _ptr(dy), dy_stride, _ptr(x), stride, code, rows, width, _ptr(mean), _ptr(rstd), _ptr(weight),
-                                       kind, _ptr(samples), count, _ptr(dx), width, _ptr(dweight), _ptr(dbias), _ptr(work), work.numel(),
+                                       kind, _ptr(samples), count, _ptr(dx), width, _ptr(dweight), _ptr(dbias), _ptr(work), room,
                                        _stream()), "he_layer_norm_backward")
     return dx, dweight, dbias
 
@@ -764,13 +763,13 @@ def he_linear_sensitivity(ctx: Ctx, x: torch.Tensor, dy: torch.Tensor, samples: 
         _vector(out_bias, outputs, torch.float32, what + "out_bias")
     _on_gpu(x, dy, samples, out, out_bias)
     if out is None:
-        out = torch.empty((outputs, inputs), dtype=torch.float32, device=x.device)
+        out = x.new_empty((outputs, inputs), dtype=torch.float32)
     if bias and out_bias is None:
-        out_bias = torch.empty(outputs, dtype=torch.float32, device=x.device)
+        out_bias = x.new_empty(outputs, dtype=torch.float32)
     aligned = _rows_aligned(x, stride, inputs) and _rows_aligned(dy, dy_stride, outputs)
-    room = _lib.he_linear_sensitivity_work_bytes(ctx.handle, code, rows, inputs, outputs, samples is not None, aligned)
-    work = torch.empty(max(room, 16), dtype=torch.uint8, device=x.device)
+    room = max(_lib.he_linear_sensitivity_work_bytes(ctx.handle, code, rows, inputs, outputs, samples is not None, aligned), 16)
+    work = x.new_empty(room, dtype=torch.uint8)
     _check(_lib.he_linear_sensitivity(ctx.handle, _ptr(x), stride, _ptr(dy), dy_stride, code, rows, inputs, outputs, _ptr(samples), count,
-                                      1 if accumulate else 0, _ptr(out), _ptr(out_bias) if bias else None, _ptr(work), work.numel(), _stream()),
+                                      1 if accumulate else 0, _ptr(out), _ptr(out_bias) if bias else None, _ptr(work), room, _stream()),
            "he_linear_sensitivity")
     return out, out_bias if bias else None

@@ -33,6 +33,29 @@ inline cudaError_t allow_shared(const void *kernel, size_t bytes) {
     return set;
 }
 
+// ---- a kernel that begins before the one ahead of it on the stream has ended ----
+//
+// Of the kernels that a call launches, the later ones may begin when every block of the one before has said next_may_begin(), and have to say
+// before_is_done() ahead of using what it leaves; one block at least says that before it ends, so that what is behind the call on the stream finds all
+// of it done (no more than one where there are others to come: blocks that wait keep their places).  A call's first kernel is launched as usual.
+__device__ __forceinline__ void next_may_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void before_is_done() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <class... P>
+cudaError_t launch_early(bool early, void (*kernel)(P...), dim3 grid, uint32_t threads, size_t shared, cudaStream_t s, const P &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = early ? 1 : 0;
+    const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, args...);
+    return rc != cudaSuccess ? rc : FEDHE_LAUNCHED();
+}
+
 template <class T>
 __device__ __forceinline__ float to_f32(T v);
 template <>

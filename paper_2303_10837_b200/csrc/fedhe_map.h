@@ -86,8 +86,10 @@ struct ColumnSumArgs {
     void *work;
 };
 size_t column_sums_work_bytes(size_t rows, size_t width, int n_sm);
-cudaError_t launch_column_sums(const ColumnSumArgs &a, int dtype, int n_sm, cudaStream_t s);
-// dst (+)= the sum of `runs` partial sums of columns, the first `width` of 3 * width words of each
+// early: beside the call's kernel before it, whose results are not used
+cudaError_t launch_column_sums(const ColumnSumArgs &a, int dtype, int n_sm, bool early, cudaStream_t s);
+// dst (+)= the sum of `runs` partial sums of columns, the first `width` of 3 * width words of each; beside the call's kernel before it, which began when
+// they were there
 cudaError_t launch_join_sums(const float *heads, uint32_t runs, size_t width, bool accumulate, float *dst, cudaStream_t s);
 
 struct LinearMapArgs {

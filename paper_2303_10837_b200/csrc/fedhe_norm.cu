@@ -379,6 +379,7 @@ constexpr uint32_t BACK_THREADS = 512;
 template <class T, int V, int HELD, bool SAMPLES>
 __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGradArgs a, const RowPlan plan, const RunsOut out, int *status) {
     constexpr int K = HELD / V;
+    next_may_begin();
     // heads and inner parts, [groups][2 planes][width] each; then the ring, where the tails go when it is done with.  Without samples the ring, then heads.
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ uint64_t bars[BACK_THREADS / 32][MOST_DEPTH];
@@ -565,6 +566,7 @@ __global__ void __launch_bounds__(SUM_COLS * SUM_WARPS) sums_kernel(const MatArg
 #pragma unroll
         for (int e = 0; e < V; e++) sum[p][e] = head[p][e] = inner[p][e] = 0.0f;
     int cut = 0;
+    next_may_begin();
     SampleWalk walk;
     walk.begin = 0;
     walk.end = INT64_MAX;
@@ -636,11 +638,13 @@ __global__ void __launch_bounds__(SUM_COLS * SUM_WARPS) sums_kernel(const MatArg
             if (p == 0 && i == 0 && blockIdx.x == 0) *out.cut(run) = all.cut;
         }
     }
+    if (blockIdx.x == 0 && blockIdx.y == 0) before_is_done();
 }
 
-// Joins all runs of a column: each warp a part of them in order, then the warps' results.
+// Joins all runs of a column: each warp a part of them in order, then the warps' results.  READY: the runs are from a kernel that is known to be done, and not from
+// the one before.
 constexpr int JOIN_WARPS = 32;
-template <bool MAGNITUDES>
+template <bool MAGNITUDES, bool READY>
 __global__ void __launch_bounds__(32 * JOIN_WARPS) sums_join_kernel(const RunsOut in, const bool accumulate, float *dst0, float *dst1) {
     __shared__ Run runs[JOIN_WARPS][33];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x / 32;
@@ -648,6 +652,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) sums_join_kernel(const RunsOu
     const size_t col = (size_t)blockIdx.x * 32 + lane;
     float *dst = plane ? dst1 : dst0;
     Run all{0.0f, 0.0f, 0.0f, 0};
+    if (!READY) before_is_done();
     const uint32_t begin = in.runs * warp / JOIN_WARPS, end = in.runs * (warp + 1) / JOIN_WARPS;
     constexpr int AHEAD = 5;                 // of 148 runs a warp has five at most
     if (col < in.width)
@@ -657,11 +662,11 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) sums_join_kernel(const RunsOu
             for (int j = 0; j < AHEAD; j++) {
                 part[j] = Run{0.0f, 0.0f, 0.0f, 0};
                 if (r0 + j >= end) continue;
-                part[j].head = in.of(r0 + j, 0, plane)[col];
+                part[j].head = __ldcg(in.of(r0 + j, 0, plane) + col);
                 if (MAGNITUDES) {
-                    part[j].inner = in.of(r0 + j, 1, plane)[col];
-                    part[j].tail = in.of(r0 + j, 2, plane)[col];
-                    part[j].cut = *in.cut(r0 + j);
+                    part[j].inner = __ldcg(in.of(r0 + j, 1, plane) + col);
+                    part[j].tail = __ldcg(in.of(r0 + j, 2, plane) + col);
+                    part[j].cut = __ldcg(in.cut(r0 + j));
                 }
             }
 #pragma unroll
@@ -675,9 +680,11 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) sums_join_kernel(const RunsOu
             runs[warp][lane] = all;
         }
     }
-    if (warp || col >= in.width) return;
-    const float v = MAGNITUDES ? fabsf(all.head) + all.inner + fabsf(all.tail) : all.head;
-    dst[col] = accumulate ? dst[col] + v : v;
+    if (warp == 0 && col < in.width) {
+        const float v = MAGNITUDES ? fabsf(all.head) + all.inner + fabsf(all.tail) : all.head;
+        dst[col] = accumulate ? dst[col] + v : v;
+    }
+    if (READY && blockIdx.x == 0) before_is_done();
 }
 
 template <class T>
@@ -693,23 +700,20 @@ inline size_t runs_bytes(size_t rows, size_t width, int planes, int n_sm) {
 }
 
 cudaError_t join_runs(const RunsOut &runs, bool magnitudes, bool accumulate, float *dst0, float *dst1, cudaStream_t s) {
-    const dim3 grid(blocks_for(runs.width, 32), runs.planes);
-    if (magnitudes) sums_join_kernel<true><<<grid, 32 * JOIN_WARPS, 0, s>>>(runs, accumulate, dst0, dst1);
-    else sums_join_kernel<false><<<grid, 32 * JOIN_WARPS, 0, s>>>(runs, accumulate, dst0, dst1);
-    return FEDHE_LAUNCHED();
+    const auto kernel = magnitudes ? sums_join_kernel<true, false> : sums_join_kernel<false, false>;
+    return launch_early(true, kernel, dim3(blocks_for(runs.width, 32), runs.planes), 32 * JOIN_WARPS, 0, s, runs, accumulate, dst0, dst1);
 }
 
 template <class T, bool X>
 cudaError_t sums(const MatArg &m, const MatArg &x, const float *mean, const float *rstd, size_t rows, size_t width, SumOver over,
-                 const int32_t *offsets, uint32_t samples, bool accumulate, float *dst0, float *dst1, void *work, int n_sm, cudaStream_t s) {
+                 const int32_t *offsets, uint32_t samples, bool accumulate, float *dst0, float *dst1, void *work, int n_sm, bool early, cudaStream_t s) {
     const bool wide = wide_rows<T>(m.p, m.stride, width) && (!X || wide_rows<T>(x.p, x.stride, width));
     // two blocks on an SM
     const unsigned cols = blocks_for(width, SUM_COLS * (wide ? WIDE<T> : 1)), most = (2 * n_sm + cols - 1) / cols, runs = sum_runs(rows, n_sm);
     const RunsOut out{static_cast<float *>(work), runs < most ? runs : most, width, X ? 2 : 1};
     const dim3 grid(cols, out.runs);
-    if (wide) sums_kernel<T, WIDE<T>, X><<<grid, SUM_COLS * SUM_WARPS, 0, s>>>(m, x, mean, rstd, rows, width, over, offsets, samples, out);
-    else sums_kernel<T, 1, X><<<grid, SUM_COLS * SUM_WARPS, 0, s>>>(m, x, mean, rstd, rows, width, over, offsets, samples, out);
-    const cudaError_t rc = FEDHE_LAUNCHED();
+    const auto kernel = wide ? sums_kernel<T, WIDE<T>, X> : sums_kernel<T, 1, X>;
+    const cudaError_t rc = launch_early(early, kernel, grid, SUM_COLS * SUM_WARPS, 0, s, m, x, mean, rstd, rows, width, over, offsets, samples, out);
     return rc != cudaSuccess ? rc : join_runs(out, over != SumOver::ALL, accumulate, dst0, dst1, s);
 }
 
@@ -776,7 +780,7 @@ cudaError_t norm_grad_of(const NormGradArgs &a, int n_sm, int *status, cudaStrea
         rc = FEDHE_LAUNCHED();
         if (rc != cudaSuccess) return rc;
     }
-    return sums<T, true>(a.dy, a.x, a.mean, a.rstd, a.rows, a.width, a.over, a.offsets, a.samples, false, a.dweight, a.dbias, a.work, n_sm, s);
+    return sums<T, true>(a.dy, a.x, a.mean, a.rstd, a.rows, a.width, a.over, a.offsets, a.samples, false, a.dweight, a.dbias, a.work, n_sm, false, s);
 }
 
 }  // namespace
@@ -787,9 +791,9 @@ cudaError_t launch_norm(const NormArgs &a, int dtype, int n_sm, int *status, cud
                               : norm_of<__half>(a, n_sm, status, s);
 }
 
-// The runs' heads, summed.
 cudaError_t launch_join_sums(const float *heads, uint32_t runs, size_t width, bool accumulate, float *dst, cudaStream_t s) {
-    return join_runs(RunsOut{const_cast<float *>(heads), runs, width, 1}, false, accumulate, dst, nullptr, s);
+    return launch_early(true, sums_join_kernel<false, true>, dim3(blocks_for(width, 32)), 32 * JOIN_WARPS, 0, s, RunsOut{const_cast<float *>(heads), runs, width, 1}, accumulate,
+                        dst, (float *)nullptr);
 }
 
 size_t norm_grad_work_bytes(size_t rows, size_t width, int n_sm) { return runs_bytes(rows, width, 2, n_sm); }
@@ -802,11 +806,11 @@ cudaError_t launch_norm_grad(const NormGradArgs &a, int dtype, int n_sm, int *st
 
 size_t column_sums_work_bytes(size_t rows, size_t width, int n_sm) { return runs_bytes(rows, width, 1, n_sm); }
 
-cudaError_t launch_column_sums(const ColumnSumArgs &a, int dtype, int n_sm, cudaStream_t s) {
+cudaError_t launch_column_sums(const ColumnSumArgs &a, int dtype, int n_sm, bool early, cudaStream_t s) {
     const MatArg none{nullptr, 0};
     const auto go = [&](auto t) {
         return sums<decltype(t), false>(a.m, none, nullptr, nullptr, a.rows, a.width, a.over, a.offsets, a.samples, a.accumulate, a.dst, nullptr,
-                                        a.work, n_sm, s);
+                                        a.work, n_sm, early, s);
     };
     return dtype == HE_F32 ? go(0.0f) : dtype == HE_BF16 ? go(__nv_bfloat16()) : go(__half());
 }

@@ -149,6 +149,39 @@ def test_masks_of_the_types_lowest_value(ctx, dtype):
     ref.close(got[keep], want, tol + ref.rounding(want, torch.float32) + 2.0 ** -126, "dlogits")
 
 
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_what_follows_a_call_finds_it_done(ctx, bias, dtype):
+    """A call's kernels overlap one another, not what comes before or behind the call on its stream."""
+    g = gen(77)
+    x, dy = (torch.randint(-2, 3, (3000, 512), generator=g, device="cuda").to(dtype) for _ in range(2))
+    alone = dy.float().abs().T @ x.float().abs()
+    cuts, source = offsets(list(range(0, 3001, 2))), (x.clone(), dy.clone())
+    pairs = (dy.float().view(1500, 2, 512).permute(0, 2, 1) @ x.float().view(1500, 2, 512)).abs().sum(0)
+    column = dy.float().view(1500, 2, 512).sum(1).abs().sum(0), dy.float().abs().sum(0)
+    _, mean, rstd = he.he_layer_norm(ctx, x)
+    back = [t.clone() for t in he.he_layer_norm_backward(ctx, dy, x, mean, rstd, samples=cuts)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for samples, want in ((None, alone), (cuts, pairs)):
+            x.copy_(source[0])
+            dy.copy_(source[1])
+            w, b = he.he_linear_sensitivity(ctx, x, dy, samples=samples, bias=bias)
+            copy = w.clone(), None if b is None else b.clone()
+            x.fill_(9.0)
+            dy.fill_(9.0)
+            w.zero_()
+            assert torch.equal(copy[0], want)
+            if bias:
+                assert torch.equal(copy[1], column[samples is None])
+        x.copy_(source[0])
+        dy.copy_(source[1])
+        got = [t.clone() for t in he.he_layer_norm_backward(ctx, dy, x, mean, rstd, samples=cuts)]
+        x.fill_(9.0)
+        dy.fill_(9.0)
+        assert all(torch.equal(a, b) for a, b in zip(got, back))
+
+
 def test_first_calls_inside_a_capture():
     code = """
 import torch, sys
