@@ -140,7 +140,7 @@ struct RunsOut {
 
 // How a row is shared out: `threads` threads (a multiple of 32), each with `held` elements, `groups` of them in a block.  A group's rows come to
 // shared memory by bulk copies, `depth` rows ahead: that many loads in registers would leave room for few warps (rows one ahead in
-// registers: 176 us for 32768 rows of 4096 in bf16, by copies ...).
+// registers: 176 us for 32768 rows of 4096 in bf16, by copies 114).
 struct RowPlan {
     uint32_t threads, groups, depth;
     uint32_t room;                                           // bytes of a row in shared memory
@@ -273,7 +273,7 @@ __device__ __forceinline__ void store_row(T *row, const F2 (&x)[K * V / 2], uint
     }
 }
 
-// Groups of threads take rows in turn; the weights stay in registers.
+// Groups of threads take rows in turn; the weights stay in registers.  One row of 4096 takes 4 us, which is a launch's.
 template <class T, int V, int HELD, int THREADS, int BLOCKS>
 __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a, const RowPlan plan, int *status) {
     constexpr int K = HELD / V;
@@ -368,6 +368,97 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
         y += step * a.y.stride;
         row += stride;
         odd ^= 1u;
+        if (++d == plan.depth) d = 0, turn ^= 1u;
+    }
+    if (lost) copies_lost(status);
+}
+
+// A warp for each row, where there are rows enough: what threads do once for a row (sums over the warp, the row's numbers, the copies) is done by 32 of
+// them and not by the 256 of a group above, of which it was two thirds of all instructions.  32768 rows of 4096 in bf16: 98 us, 5.5 TB/s.  The weights are in shared memory, in packs of four, [weight, bias][fours of a pack][packs].
+template <class T, int HELD, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 1) norm_warp_kernel(const NormArgs a, const RowPlan plan, int *status) {
+    constexpr int V = WIDE<T>, K = HELD / V, FOURS = V / 4;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ uint64_t bars[WARPS][MOST_DEPTH];
+    const uint32_t warp = threadIdx.x / 32, t = threadIdx.x & 31u, width = (uint32_t)a.width, packs = width / V;
+    const uint32_t step = gridDim.x * plan.groups, first = blockIdx.x * plan.groups + warp, count = (uint32_t)a.rows;
+    const Rows<T, true> rows(a.x, a.rows, width);
+    float4 *weights = reinterpret_cast<float4 *>(ring);
+    uint8_t *mine = ring + (size_t)width * 2 * sizeof(float) + (size_t)warp * plan.depth * plan.room;
+    const uint32_t mine_at = shared_at(mine), bar = shared_at(&bars[warp][0]);
+    uint32_t asked = warp < plan.groups ? first : count;
+    uintptr_t asked_at = rows.at(first);
+    const uintptr_t stride = (uintptr_t)step * rows.pitch;
+    const auto ask = [&](uint32_t d) {
+        if (asked >= count) return;
+        copies_begin(bar + d * 8, rows.bytes);
+        rows.copy(asked_at, mine_at + d * plan.room, bar + d * 8);
+        asked += step;
+        asked_at += stride;
+    };
+    if (t == 0) {
+        for (uint32_t d = 0; d < plan.depth; d++) barrier_init(bar + d * 8, 1);
+        barriers_ready();
+        for (uint32_t d = 0; d < plan.depth; d++) ask(d);
+    }
+    for (uint32_t c = threadIdx.x; c < width; c += 32 * WARPS) {
+        const uint32_t at = (c % V / 4 * packs + c / V) * 4 + c % 4;
+        float *w = reinterpret_cast<float *>(weights);
+        w[at] = a.weight ? load_weight(a.weight, a.weight_type, c) : 1.0f;
+        w[width + at] = a.bias ? load_weight(a.bias, a.weight_type, c) : 0.0f;
+    }
+    __syncthreads();
+    if (warp >= plan.groups) return;
+    const float all = (float)width, part = 1.0f / all;
+    uint32_t d = 0, turn = 0;
+    T *y = static_cast<T *>(a.y.p) + (size_t)first * a.y.stride;
+    bool lost = false;                                       // a copy did not come: none is waited for any more
+    for (uint32_t r = first; r < count; r += step) {
+        if (!lost && !copies_done(bar + d * 8, turn)) lost = true;
+        F2 x[HELD / 2], s[4] = {F2(0.0f), F2(0.0f), F2(0.0f), F2(0.0f)}, q[4] = {F2(0.0f), F2(0.0f), F2(0.0f), F2(0.0f)};
+        const T *in = reinterpret_cast<const T *>(mine + d * plan.room) + t * V;
+#pragma unroll
+        for (int k = 0; k < K; k++) {
+            if (k * 32 + t < packs) {
+                const Pack<T, V> p = load_pack<T, V>(in + k * 32 * V);
+#pragma unroll
+                for (int i = 0; i < V / 2; i++) {
+                    x[k * (V / 2) + i] = two_of(p, i);
+                    s[i % 4] = s[i % 4] + x[k * (V / 2) + i];
+                }
+            }
+        }
+        // squares about what is the mean but for a rounding
+        const float sum = warp_sum(((s[0] + s[1]) + (s[2] + s[3])).sum()), about = sum * part;
+        if (t == 0) ask(d);                                  // the row is in registers: its place takes another
+#pragma unroll
+        for (int k = 0; k < K; k++)
+            if (k * 32 + t < packs) {
+#pragma unroll
+                for (int i = 0; i < V / 2; i++) {
+                    const F2 z = x[k * (V / 2) + i] + F2(-about);
+                    q[i % 4] = fma2(z, z, q[i % 4]);
+                }
+            }
+        const float squares = warp_sum(((q[0] + q[1]) + (q[2] + q[3])).sum()), mean = quotient(sum, all, part), rstd = inverse_root(fmaf(squares, part, a.eps));
+        if (t == 0) {
+            a.mean[r] = mean;
+            a.rstd[r] = rstd;
+        }
+#pragma unroll
+        for (int k = 0; k < K; k++)
+            if (k * 32 + t < packs) {
+                Pack<T, V> o;
+#pragma unroll
+                for (int f = 0; f < FOURS; f++) {
+                    const float4 w = weights[f * packs + k * 32 + t], b = weights[width / 4 + f * packs + k * 32 + t];
+                    const int i = k * (V / 2) + f * 2;
+                    set_two(o, f * 2, fma2((x[i] + F2(-mean)) * F2(rstd), F2(w.x, w.y), F2(b.x, b.y)));
+                    set_two(o, f * 2 + 1, fma2((x[i + 1] + F2(-mean)) * F2(rstd), F2(w.z, w.w), F2(b.z, b.w)));
+                }
+                store_pack<T, V>(y + (k * 32 + t) * V, o);
+            }
+        y += step * a.y.stride;
         if (++d == plan.depth) d = 0, turn ^= 1u;
     }
     if (lost) copies_lost(status);
@@ -732,11 +823,35 @@ bool norm_go(const NormArgs &a, int n_sm, int *status, cudaStream_t s, cudaError
     return true;
 }
 
+// With fewer than eight rows for each warp the groups below, which are more threads to a row, are as fast or faster (8192 rows of 4096 in fp32: 53 and 51 us,
+// 32768: 182 and 188; in bf16 35 and 37, 98 and 119; 32768 rows of 768 in bf16 27 and 35).
+template <class T, int HELD, int WARPS>
+bool norm_warp_go(const NormArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
+    if (a.width > 32 * HELD || a.rows < (size_t)8 * WARPS * n_sm) return false;
+    RowPlan plan;
+    plan.threads = 32;
+    plan.room = (uint32_t)(a.width * sizeof(T));
+    const size_t kept = a.width * 2 * sizeof(float), places = (MOST_SHARED - kept) / plan.room;
+    plan.groups = (uint32_t)(places < WARPS ? places : WARPS);
+    plan.depth = (uint32_t)(places / plan.groups < MOST_DEPTH ? places / plan.groups : MOST_DEPTH);
+    const auto kernel = norm_warp_kernel<T, HELD, WARPS>;
+    const size_t bytes = kept + (size_t)plan.groups * plan.depth * plan.room;
+    rc = allow_shared(reinterpret_cast<const void *>(kernel), bytes);
+    if (rc != cudaSuccess) return true;
+    kernel<<<n_sm, 32 * WARPS, bytes, s>>>(a, plan, status);
+    rc = FEDHE_LAUNCHED();
+    return true;
+}
+
 template <class T>
 cudaError_t norm_of(const NormArgs &a, int n_sm, int *status, cudaStream_t s) {
     if (a.rows == 0) return cudaSuccess;
     const bool wide = wide_rows<T>(a.x.p, a.x.stride, a.width) && wide_rows<T>(a.y.p, a.y.stride, a.width);
     cudaError_t rc;
+    // Up to 512 columns a group below is a warp as well.
+    if (wide && a.width > 512 &&
+        (norm_warp_go<T, 32, 24>(a, n_sm, status, s, rc) || norm_warp_go<T, 64, 16>(a, n_sm, status, s, rc) || norm_warp_go<T, 128, 12>(a, n_sm, status, s, rc)))
+        return rc;
     if (wide ? norm_go<T, WIDE<T>, 16, 256, 3>(a, n_sm, status, s, rc) : norm_go<T, 1, 16, 256, 3>(a, n_sm, status, s, rc)) return rc;
     if (wide ? norm_go<T, WIDE<T>, 16, 1024, 1>(a, n_sm, status, s, rc) : norm_go<T, 1, 16, 1024, 1>(a, n_sm, status, s, rc)) return rc;
     if (wide) norm_long_kernel<T, WIDE<T>><<<(unsigned)a.rows, row_threads(a.width / WIDE<T>), 0, s>>>(a);

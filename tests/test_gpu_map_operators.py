@@ -196,6 +196,26 @@ def test_layer_norm(ctx, dtype, rows, width, weights):
     assert out is same and torch.equal(same, he.he_layer_norm(ctx, x, w, b, eps=1e-5)[0])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,width", [(30000, 520), (28500, 1024), (20000, 1032), (19001, 2048), (14300, 2056), (14300, 4096)])
+def test_layer_norm_of_many_rows(ctx, dtype, rows, width):
+    g, t = gen(rows + width), ref.DTYPES[dtype]
+    x = (randn(g, rows, width) * 2 + randn(g, width)).to(t)
+    w, b = randn(g, width), randn(g, width).to(t)
+    for weight, bias in ((w, w), (None, b), (None, None)):
+        y, mean, rstd = he.he_layer_norm(ctx, x, weight, bias)
+        for lo in range(0, rows, 5000):
+            (wy, ty), (wm, tm), (wr, tr) = ref.norm(x[lo:lo + 5000], weight, bias, 1e-5)
+            ref.close(y[lo:lo + 5000], wy, ty + ref.rounding(wy, t), "y")
+            ref.close(mean[lo:lo + 5000], wm, tm, "mean")
+            ref.close(rstd[lo:lo + 5000], wr, tr, "rstd")
+    out, _, _ = he.he_layer_norm(ctx, x, w, w)
+    room = torch.zeros(rows, width + 8, dtype=t, device="cuda")
+    room[:, :width] = x
+    got = he.he_layer_norm(ctx, room[:, :width], w, w, out=room[:, :width])[0]
+    assert torch.equal(got, out) and (room[:, width:] == 0).all()
+
+
 def test_layer_norm_of_equal_values_and_of_rows_that_are_not_finite(ctx):
     x = torch.full((4, 300), 3.0, device="cuda")
     x[1, 5], x[2, 7] = float("nan"), INF
