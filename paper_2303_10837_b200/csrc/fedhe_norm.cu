@@ -466,7 +466,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) norm_warp_kernel(const NormArgs
 
 // The backward pass.  A block takes a run of rows, its groups parts of it in order; sums over rows stay in registers, and go to shared
 // memory where a sample ends.  What the block leaves is a run's head, inner part and tail of every column (see Run).
-constexpr uint32_t BACK_THREADS = 512;
+constexpr uint32_t BACK_THREADS = 256;
 template <class T, int V, int HELD, bool SAMPLES>
 __global__ void __launch_bounds__(BACK_THREADS, 1) norm_grad_kernel(const NormGradArgs a, const RowPlan plan, const RunsOut out, int *status) {
     constexpr int K = HELD / V;
@@ -860,12 +860,12 @@ cudaError_t norm_of(const NormArgs &a, int n_sm, int *status, cudaStream_t s) {
 }
 
 template <class T, int V, int HELD, bool SAMPLES>
-bool norm_grad_go(const NormGradArgs &a, uint32_t depth, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
+bool norm_grad_go(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
     RowPlan plan;
     const size_t t = ((a.width + HELD - 1) / HELD + 31) / 32 * 32;
     if (t > BACK_THREADS) return false;
     const size_t plane = (BACK_THREADS / t) * 2 * a.width * sizeof(float), kept = SAMPLES ? (2 * plane + 15) / 16 * 16 : 0;
-    if (kept > MOST_SHARED || !plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, MOST_SHARED - kept, plan) || plan.depth < depth) return false;
+    if (kept > MOST_SHARED || !plan_row(a.width, sizeof(T), BACK_THREADS, HELD, 2, MOST_SHARED - kept, plan)) return false;
     const auto kernel = norm_grad_kernel<T, V, HELD, SAMPLES>;
     const size_t copies = (size_t)plan.groups * plan.depth * 2 * plan.room, bytes = kept + (copies > plane ? copies : plane);
     const RunsOut out{static_cast<float *>(a.work), sum_runs(a.rows, n_sm), a.width, 2};
@@ -877,10 +877,14 @@ bool norm_grad_go(const NormGradArgs &a, uint32_t depth, int n_sm, int *status, 
     return true;
 }
 
+// Elements of a thread: 32 for long rows and, of 16-bit types, for much work, of which each row's own instructions then are a smaller part; 16 where what comes
+// before and behind the rows counts more, or memory (16384 rows of 4096 in bf16: 108 us with samples and 86 without, with 16 elements 139 and 109; 4096 rows of 1024:
+// 31 and 22, 27 and 19; 16384 rows of 4096 in fp32: 164 and 151, 160 and 149).
 template <class T, int V>
 bool norm_grad_held(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
-    if (a.over == SumOver::SAMPLES) return norm_grad_go<T, V, 16, true>(a, 2, n_sm, status, s, rc) || norm_grad_go<T, V, 8, true>(a, 2, n_sm, status, s, rc) || norm_grad_go<T, V, 16, true>(a, 1, n_sm, status, s, rc);
-    return norm_grad_go<T, V, 16, false>(a, 1, n_sm, status, s, rc);
+    const bool many = V > 1 && sizeof(T) == 2 && a.width > 512 && a.rows * a.width >= (size_t)1 << 23;
+    if (a.over == SumOver::SAMPLES) return (!many && norm_grad_go<T, V, 16, true>(a, n_sm, status, s, rc)) || norm_grad_go<T, V, 32, true>(a, n_sm, status, s, rc);
+    return (!many && norm_grad_go<T, V, 16, false>(a, n_sm, status, s, rc)) || norm_grad_go<T, V, 32, false>(a, n_sm, status, s, rc);
 }
 
 template <class T>
