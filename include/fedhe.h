@@ -9,7 +9,8 @@
  *   [W_glob] = sum_i a_i [[M (.) W_i]] + sum_i a_i ((1-M) (.) W_i), "Step 2"
  *   of Selective Parameter Encryption (mask = ratio p of the most sensitive
  *   parameters), and the framework API table (key_gen, enc, he_aggregate,
- *   dec; flatten/reshape stay with the caller).
+ *   dec; flatten/reshape stay with the caller); below them what a client
+ *   computes its sensitivity map with ("Step 1").
  *
  * Conventions
  *   - Every call returns an int: HE_OK (0) or a negative HE_ERR_* code; no
@@ -99,8 +100,8 @@ int he_ctx_create(const he_params *params, he_ctx **out);
 int he_ctx_destroy(he_ctx *ctx);
 /* Synchronises the device, returns the sticky status (HE_OK; HE_ERR_OVERFLOW,
  * an encoded coefficient out of range or an input that is not finite;
- * HE_ERR_CUDA, a copy inside a kernel did not arrive and results since the
- * last call are incomplete) in *status and clears it. */
+ * HE_ERR_CUDA, a copy or a product inside a kernel did not arrive and results
+ * since the last call are incomplete) in *status and clears it. */
 int he_ctx_status(he_ctx *ctx, int *status);
 /* Pre-sizes the library-owned work buffers for encryptions/decryptions of up
  * to max_k encrypted parameters so that later calls allocate nothing.
