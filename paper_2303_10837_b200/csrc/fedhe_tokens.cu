@@ -3,7 +3,9 @@
 //   lse = m + ln s,  m = max z,  s = sum e^(z - m);   log p_y = (z_y - m) - ln s;   H = ln s - (sum e^(z - m) (z - m)) / s
 //   dz_j = sum_i g_i (d_{j,t_i} - p_j) - g_H p_j (log p_j + H)        t_i: the target and the alternatives, g_i their gradients
 //
-// Both directions are bounded by reading (and writing) the logits once.
+// Both directions would be bounded by reading (and writing) the logits once.  The gradient is: 8192 x 32768 in bf16 take 170 us, 6.3 TB/s.  Log
+// probabilities of 2048 x 131072 in bf16 take 138 us with eight alternatives, 3.9 TB/s, and 111 without, which a quarter of the arithmetic does
+// not change: rows are read side by side, one for each block.
 #include <cooperative_groups.h>
 
 #include "fedhe_map.cuh"
@@ -202,7 +204,7 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
 
 // Rows by clusters of C blocks (C = 1: by blocks), which take a row's pieces in turn; each warp has its part of a piece, PIECE_BYTES in a row, and
 // asks for its parts by bulk copies, DEPTH ahead and on into the next row (asked for in registers, one ahead: 307 us for 2048 x
-// 131072 in bf16 with eight alternatives; so 193).  Candidates for the alternatives are values that are not below a bound on the top-th value,
+// 131072 in bf16 with eight alternatives; so 193 then).  Candidates for the alternatives are values that are not below a bound on the top-th value,
 // raised after 1, 4, 16, ... pieces, between which some three times as many candidates come as are wanted.
 template <class T, bool TOP>
 __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C, int *status) {
