@@ -4,7 +4,7 @@
 //   dz_j = sum_i g_i (d_{j,t_i} - p_j) - g_H p_j (log p_j + H)        t_i: the target and the alternatives, g_i their gradients
 //
 // Both directions would be bounded by reading (and writing) the logits once.  The gradient is: 8192 x 32768 in bf16 take 170 us, 6.3 TB/s.  Log
-// probabilities of 2048 x 131072 in bf16 take 138 us with eight alternatives, 3.9 TB/s, and 111 without, which a quarter of the arithmetic does
+// probabilities of 2048 x 131072 in bf16 take 135 us with eight alternatives, 4.0 TB/s, and 111 without, which a quarter of the arithmetic does
 // not change: rows are read side by side, one for each block.
 #include <cooperative_groups.h>
 
@@ -19,7 +19,7 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float FAR = -1e20f;             // exponents stop here: 2^FAR is 0, and FAR times what a row sums up to or a gradient is no infinity
 constexpr int PACKS = 4;                  // of 16 bytes, that a thread has of a piece
-constexpr uint32_t FOUND = 512;           // candidates that a block can hold
+constexpr uint32_t PLACES = 256;          // for candidates of a warp
 constexpr uint32_t DEPTH = 3;             // pieces that a warp asks for ahead
 constexpr uint32_t PIECE_BYTES = 32 * PACKS * 16;      // of a warp
 
@@ -124,27 +124,48 @@ __device__ __forceinline__ float top_of<__half>(const Pack<__half, 8> &p) {
 }
 
 struct Found {
-    uint64_t key[FOUND];
-    uint64_t best[HE_MAX_TOP];
-    uint32_t count, bound[8];
+    uint64_t best[2][HE_MAX_TOP];            // the highest so far, in order: one is written from the other and from the candidates
+    uint32_t count[8], bound[8];             // each warp's candidates
     uint64_t most[8];
+    uint32_t now, held;                      // for the cluster's first block: which of `best`, and how many
 };
 
-// The `top` highest of key[0 .. n) in order, to its front; returns how many there are.  By the whole block.
-__device__ __forceinline__ uint32_t keep_best(Found &f, uint32_t n, uint32_t top) {
+// The `top` highest of what `best` holds and of the warps' candidates, to the other `best`; returns how many there are.  By the whole block, after a
+// barrier; `lost` where a warp had more candidates than places.
+__device__ __forceinline__ uint32_t keep_best(Found &f, const uint64_t *key, uint32_t now, uint32_t held, uint32_t top, bool &lost) {
+    const uint32_t warps = blockDim.x / 32;
+    uint32_t n = held;
+    for (uint32_t w = 0; w < warps; w++) {
+        lost |= f.count[w] > PLACES;
+        n += min(f.count[w], PLACES);
+    }
     for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-        const uint64_t mine = f.key[i];
+        uint64_t mine = 0;
+        if (i < held) {
+            mine = f.best[now][i];
+        } else {
+            uint32_t at = i - held;
+            for (uint32_t w = 0; w < warps; w++) {
+                const uint32_t c = min(f.count[w], PLACES);
+                if (at < c) {
+                    mine = key[w * PLACES + at];
+                    break;
+                }
+                at -= c;
+            }
+        }
         uint32_t above = 0;
-#pragma unroll 8
-        for (uint32_t j = 0; j < n; j++) above += f.key[j] > mine;
-        if (above < top) f.best[above] = mine;
+#pragma unroll 4
+        for (uint32_t j = 0; j < held; j++) above += f.best[now][j] > mine;
+        for (uint32_t w = 0; w < warps; w++) {
+            const uint32_t c = min(f.count[w], PLACES);
+#pragma unroll 4
+            for (uint32_t j = 0; j < c; j++) above += key[w * PLACES + j] > mine;
+        }
+        if (above < top) f.best[now ^ 1u][above] = mine;
     }
     __syncthreads();
-    const uint32_t kept = n < top ? n : top;
-    for (uint32_t i = threadIdx.x; i < kept; i += blockDim.x) f.key[i] = f.best[i];
-    if (threadIdx.x == 0) f.count = kept;
-    __syncthreads();
-    return kept;
+    return n < top ? n : top;
 }
 
 // A lower bound of the order of the top-th value of what the block's threads hold, given each thread's maximum: in each warp the
@@ -167,8 +188,9 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
 // The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are as high as the
 // bound that the candidates have no room, or NaN is among the highest.
 template <class T>
-__device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t first, uint32_t step, uint32_t pieces, uint32_t top) {
+__device__ __noinline__ uint32_t search(Found &f, uint32_t now, const T *p, uint32_t count, uint32_t first, uint32_t step, uint32_t pieces, uint32_t top) {
     constexpr int V = WIDE<T>;
+    const Row<T> row(p, count);
     const uint32_t NT = blockDim.x;
     uint64_t below = ~0ull;
     uint32_t n = 0;
@@ -179,11 +201,11 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
             for (uint32_t i = 0; i < PACKS; i++) {
                 const uint32_t v = (c * PACKS + i) * NT + threadIdx.x;
                 if (v >= row.vectors) break;
-                const Pack<T, V> p = row.load(v);
+                const Pack<T, V> z = row.load(v);
 #pragma unroll
                 for (int e = 0; e < V; e++) {
                     const int64_t j = row.first(v) + e;
-                    const uint64_t k = key_of(to_f32(p.v[e]), (uint32_t)j);
+                    const uint64_t k = key_of(to_f32(z.v[e]), (uint32_t)j);
                     if (j >= 0 && j < (int64_t)row.n && k < below && k > best) best = k;
                 }
             }
@@ -194,10 +216,9 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
         for (uint32_t w = 0; w < NT / 32; w++) best = max(best, f.most[w]);
         __syncthreads();
         if (best == 0) break;                // a key of an element is not 0: its index is below 2^32 - 1
-        if (threadIdx.x == 0) f.key[n] = best;
+        if (threadIdx.x == 0) f.best[now][n] = best;
         below = best;
     }
-    if (threadIdx.x == 0) f.count = n;
     __syncthreads();
     return n;
 }
@@ -205,7 +226,8 @@ __device__ __noinline__ uint32_t search(Found &f, const Row<T> &row, uint32_t fi
 // Rows by clusters of C blocks (C = 1: by blocks), which take a row's pieces in turn; each warp has its part of a piece, PIECE_BYTES in a row, and
 // asks for its parts by bulk copies, DEPTH ahead and on into the next row (asked for in registers, one ahead: 307 us for 2048 x
 // 131072 in bf16 with eight alternatives; so 193 then).  Candidates for the alternatives are values that are not below a bound on the top-th value,
-// raised after 1, 4, 16, ... pieces, between which some three times as many candidates come as are wanted.
+// at first from the first piece's, raised after 2, 8, 32, ... pieces, between which some three times as many candidates come as are wanted (after 1, 4, 16: with
+// eight alternatives up to 2 us more, with 64 up to 7 % less; after 2, 16, 128: with 64 a third more).
 template <class T, bool TOP>
 __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a, const uint32_t C, int *status) {
     constexpr int V = WIDE<T>;
@@ -221,6 +243,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
     // whole 16 bytes of the matrix: no copy reaches outside
     const uintptr_t low = (base + 15) & ~(uintptr_t)15, high = (base + (rows - 1) * pitch + (size_t)n * sizeof(T)) & ~(uintptr_t)15;
     uint8_t *room = ring + warp * DEPTH * PIECE_BYTES;
+    uint64_t *key = reinterpret_cast<uint64_t *>(ring + NT / 32 * DEPTH * PIECE_BYTES), *my_key = key + warp * PLACES;
     const uint32_t room_at = shared_at(room), bar = shared_at(&bars[warp][0]);
     // by a warp's first lane: the piece to ask for next, where it and its row's end are, and the row's pieces
     uint32_t asked_row = first_row, asked = rank, asked_pieces = 0;
@@ -258,16 +281,12 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         const Row<T> row(reinterpret_cast<const T *>(base + r * pitch), n);
         const uint32_t pieces = (row.vectors + NT * PACKS - 1) / (NT * PACKS);
         Soft q{-INFINITY, F2(0.0f), F2(0.0f)};
-        uint32_t held = 0, round = 0;
+        uint32_t held = 0, now = 0, round = 0, fresh = 0;      // fresh: this warp's candidates
         // vectors that lie in the row as a whole
         const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V;
         float from = -INFINITY;              // what a candidate has at least
-        uint32_t raise = 0;                  // the piece after which the bound is raised next
+        uint32_t raise = 1;                  // the piece after which the bound is raised next
         bool lost = false;
-        if (TOP) {
-            if (tid == 0) f.count = 0;
-            __syncthreads();
-        }
         for (uint32_t c = rank; c < pieces; c += C, round++) {
             if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
             Pack<T, V> z[PACKS];
@@ -305,28 +324,23 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
                 if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
                 // threads that have a candidate, few: the warp looks through the values of one after the other, a lane at each value
                 for (uint32_t who = __ballot_sync(0xffffffffu, m >= from); who; who &= who - 1) {
-                    const uint32_t l = __ffs(who) - 1, i = lane / V, e = lane % V;
-                    const int64_t j = row.first(v0 - lane + i * 32 + l) + e;
-                    bool hit = i < PACKS && j >= 0 && j < (int64_t)row.n;
+                    const uint32_t l = __ffs(who) - 1, i = lane / V, e = lane % V, j = (v0 - lane + i * 32 + l) * V + e - row.shift;      // outside the row: above n
+                    bool hit = i < PACKS && j < n;
                     const float x = !hit ? 0.0f : to_f32(inside ? reinterpret_cast<const T *>(in - lane * 16 + (i * 32 + l) * 16)[e] : row.p[j]);
                     hit = hit && x >= from;
-                    const uint32_t hits = __ballot_sync(0xffffffffu, hit);
-                    uint32_t at = 0;
-                    if (lane == 0) at = atomicAdd(&f.count, __popc(hits));
-                    at = __shfl_sync(0xffffffffu, at, 0) + __popc(hits & ((1u << lane) - 1));
-                    if (hit && at < FOUND) f.key[at] = key_of(x, (uint32_t)j);
-                    __syncwarp();
+                    const uint32_t hits = __ballot_sync(0xffffffffu, hit), at = fresh + __popc(hits & ((1u << lane) - 1));
+                    if (hit && at < PLACES) my_key[at] = key_of(x, j);
+                    fresh += __popc(hits);
                 }
                 if (round == raise || c + C >= pieces) {
                     raise = raise * 4 + 3;
+                    if (lane == 0) f.count[warp] = fresh;
                     __syncthreads();
-                    const uint32_t found = f.count;
-                    __syncthreads();
-                    lost |= found > FOUND;
-                    held = keep_best(f, min(found, FOUND), a.top);
+                    held = keep_best(f, key, now, held, a.top, lost);
+                    now ^= 1u;
+                    fresh = 0;
                     // later pieces have higher indices: with enough candidates a value equal to the lowest of them is too late
-                    if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.key[a.top - 1] >> 32) + 1));
-                    __syncthreads();
+                    if (held == a.top) from = fmaxf(from, value_of((uint32_t)(f.best[now][a.top - 1] >> 32) + 1));
                 }
             }
             __syncwarp();
@@ -334,7 +348,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
             if (++d == DEPTH) d = 0, turn ^= 1u;
         }
         // too many candidates; or too few, where NaN is among the row's highest
-        if (TOP && (lost || held < a.top)) held = search<T>(f, row, rank, C, pieces, a.top);
+        if (TOP && (lost || held < a.top)) held = search<T>(f, now, row.p, n, rank, C, pieces, a.top);
         // the threads' sums, then the warps'
         q.join_warp();
         if (lane == 0) {
@@ -356,6 +370,10 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         }
         if (C > 1) {
             cg::cluster_group cluster = cg::this_cluster();
+            if (TOP && tid == 0) {
+                f.now = now;
+                f.held = held;
+            }
             cluster.sync();
             if (rank == 0) {
                 if (tid < 32) {
@@ -365,14 +383,15 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
                     q.join_warp();
                 }
                 if (TOP) {
-                    for (uint32_t i = tid + a.top; i < C * a.top; i += NT) {
+                    // the blocks' alternatives beside one another, as the first warps' candidates
+                    for (uint32_t i = tid; i < C * a.top; i += NT) {
                         const Found &there = *cluster.map_shared_rank(&f, i / a.top);
-                        f.key[i] = i % a.top < there.count ? there.key[i % a.top] : 0;
+                        key[i] = i % a.top < there.held ? there.best[there.now][i % a.top] : 0;
                     }
-                    for (uint32_t i = tid; i < a.top; i += NT)
-                        if (i >= held) f.key[i] = 0;
+                    if (lane == 0) f.count[warp] = warp * PLACES < C * a.top ? min(C * a.top - warp * PLACES, PLACES) : 0;
                     __syncthreads();
-                    keep_best(f, C * a.top, a.top);
+                    keep_best(f, key, now, 0, a.top, lost);
+                    now ^= 1u;
                 }
             }
             cluster.sync();                  // nobody goes on while its memory is read
@@ -398,7 +417,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         }
         if (TOP) {
             for (uint32_t i = tid; i < a.top; i += NT) {
-                const uint64_t k = f.key[i];
+                const uint64_t k = f.best[now][i];
                 a.top_ids[(size_t)r * a.top + i] = (int64_t)(0xffffffffu - (uint32_t)k);
                 a.top_logp[(size_t)r * a.top + i] = none ? -INFINITY : (value_of((uint32_t)(k >> 32)) - b) - ln;
             }
@@ -418,9 +437,10 @@ inline uint32_t row_threads(size_t bytes, size_t rows, int n_sm) {
 
 template <class T>
 cudaError_t log_probs_of(const LogProbsArgs &a, int n_sm, int *status, cudaStream_t s) {
-    const uint32_t nt = row_threads(a.vocab * sizeof(T), a.rows, n_sm);
+    // a warp has 32 values for a bound at once
+    const uint32_t least = a.top > 32 ? 64 : 32, wanted = row_threads(a.vocab * sizeof(T), a.rows, n_sm), nt = wanted < least ? least : wanted;
     const size_t pieces = (a.vocab * sizeof(T) + 15 + (size_t)nt * PACKS * 16 - 1) / ((size_t)nt * PACKS * 16);
-    const uint32_t bytes = nt / 32 * DEPTH * PIECE_BYTES;
+    const uint32_t bytes = nt / 32 * (DEPTH * PIECE_BYTES + (a.top ? PLACES * 8 : 0));
     // blocks that an SM holds: 768 threads by the registers, and shared memory
     uint32_t held = 768 / nt;
     const uint32_t by_memory = (uint32_t)((222u << 10) / (bytes + (a.top ? sizeof(Found) : 0) + 1536));
