@@ -127,7 +127,7 @@ struct Found {
     uint64_t best[2][HE_MAX_TOP];            // the highest so far, in order: one is written from the other and from the candidates
     uint32_t count[8], bound[8];             // each warp's candidates
     uint64_t most[8];
-    uint32_t now, held;                      // for the cluster's first block: which of `best`, and how many
+    uint32_t now, held;                      // which of `best`, and how many are there: for the cluster's first block
 };
 
 // The `top` highest of what `best` holds and of the warps' candidates, to the other `best`; returns how many there are.  By the whole block, after a
@@ -185,8 +185,39 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
     return low;
 }
 
-// The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are as high as the
-// bound that the candidates have no room, or NaN is among the highest.
+// Fewer than `top` values were above the order `edge`, which the first piece alone has so many values from on: the rest are of that order, and those with
+// the lowest indices lie in that piece.  By a warp; returns how many there are then.
+template <class T>
+__device__ __noinline__ uint32_t fill(Found &f, uint32_t now, uint32_t held, uint32_t edge, const T *p, uint32_t count, uint32_t first, uint32_t top) {
+    constexpr int V = WIDE<T>;
+    const Row<T> row(p, count);
+    const uint32_t lane = threadIdx.x & 31u, piece = blockDim.x * PACKS;
+    for (uint32_t at = first * piece; at < (first + 1) * piece && at < row.vectors && held < top; at += 32) {
+        const uint32_t v = at + lane;
+        uint32_t like = 0;
+        if (v < row.vectors) {
+            const Pack<T, V> z = row.load(v);
+#pragma unroll
+            for (int e = 0; e < V; e++) {
+                const int64_t j = row.first(v) + e;
+                like |= (uint32_t)(j >= 0 && j < (int64_t)row.n && order_of(to_f32(z.v[e])) == edge) << e;
+            }
+        }
+        uint32_t upto = __popc(like);
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const uint32_t before = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= (uint32_t)o) upto += before;
+        }
+        for (uint32_t to = held + upto - __popc(like); like && to < top; like &= like - 1, to++)
+            f.best[now][to] = (uint64_t)edge << 32 | (0xffffffffu - (uint32_t)(row.first(v) + __ffs(like) - 1));
+        held += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return held < top ? held : top;
+}
+
+// The alternatives of the pieces first, first + step, ... of a row by one search for each of them: where so many values are above the bound that the
+// candidates have no room, as in a row that ascends.
 template <class T>
 __device__ __noinline__ uint32_t search(Found &f, uint32_t now, const T *p, uint32_t count, uint32_t first, uint32_t step, uint32_t pieces, uint32_t top) {
     constexpr int V = WIDE<T>;
@@ -225,7 +256,7 @@ __device__ __noinline__ uint32_t search(Found &f, uint32_t now, const T *p, uint
 
 // Rows by clusters of C blocks (C = 1: by blocks), which take a row's pieces in turn; each warp has its part of a piece, PIECE_BYTES in a row, and
 // asks for its parts by bulk copies, DEPTH ahead and on into the next row (asked for in registers, one ahead: 307 us for 2048 x
-// 131072 in bf16 with eight alternatives; so 193 then).  Candidates for the alternatives are values that are not below a bound on the top-th value,
+// 131072 in bf16 with eight alternatives; so 193 then).  Candidates for the alternatives are values above a bound of the top-th value,
 // at first from the first piece's, raised after 2, 8, 32, ... pieces, between which some three times as many candidates come as are wanted (after 1, 4, 16: with
 // eight alternatives up to 2 us more, with 64 up to 7 % less; after 2, 16, 128: with 64 a third more).
 template <class T, bool TOP>
@@ -284,7 +315,8 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         uint32_t held = 0, now = 0, round = 0, fresh = 0;      // fresh: this warp's candidates
         // vectors that lie in the row as a whole
         const uint32_t whole_from = row.shift ? 1 : 0, whole_to = (row.n + row.shift) / V;
-        float from = -INFINITY;              // what a candidate has at least
+        uint32_t edge = 0;                   // an order that the first piece has `top` values from on
+        float from = -INFINITY;              // what a candidate has at least: above that, and later above the top-th value so far
         uint32_t raise = 1;                  // the piece after which the bound is raised next
         bool lost = false;
         for (uint32_t c = rank; c < pieces; c += C, round++) {
@@ -321,7 +353,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
 #pragma unroll
                 for (int e = 0; e < V / 2; e++) q.add(two_of(z[i], e), b);
             if (TOP) {
-                if (round == 0) from = value_of(bound_of_top(f, order_of(m), a.top));
+                if (round == 0) edge = bound_of_top(f, order_of(m), a.top), from = value_of(edge + 1);
                 // threads that have a candidate, few: the warp looks through the values of one after the other, a lane at each value
                 for (uint32_t who = __ballot_sync(0xffffffffu, m >= from); who; who &= who - 1) {
                     const uint32_t l = __ffs(who) - 1, i = lane / V, e = lane % V, j = (v0 - lane + i * 32 + l) * V + e - row.shift;      // outside the row: above n
@@ -347,8 +379,17 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
             if (lane == 0) ask(d);
             if (++d == DEPTH) d = 0, turn ^= 1u;
         }
-        // too many candidates; or too few, where NaN is among the row's highest
-        if (TOP && (lost || held < a.top)) held = search<T>(f, now, row.p, n, rank, C, pieces, a.top);
+        if (TOP) {
+            if (held < a.top && rank < pieces) {
+                if (warp == 0) {
+                    const uint32_t with = fill<T>(f, now, held, edge, row.p, n, rank, a.top);
+                    if (lane == 0) f.held = with;
+                }
+                __syncthreads();
+                held = f.held;
+            }
+            if (lost) held = search<T>(f, now, row.p, n, rank, C, pieces, a.top);
+        }
         // the threads' sums, then the warps'
         q.join_warp();
         if (lane == 0) {

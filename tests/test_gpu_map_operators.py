@@ -82,6 +82,25 @@ def test_alternatives_of_equal_and_of_sorted_values(ctx, V):
         check_log_probs(ctx, z, y, top)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,V,top", [(3, 100, 64), (5, 9000, 20), (2, 131072, 64), (900, 5003, 8), (1, 20000, 1)])
+def test_alternatives_among_few_values(ctx, dtype, rows, V, top):
+    """Masks that leave fewer tokens than alternatives, equal logits, logits of few sizes: the lowest indices of equal ones."""
+    g, t = gen(V + top), ref.DTYPES[dtype]
+    z = randn(g, rows, V) * 2
+    y = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    sparse = torch.rand(rows, V, generator=g, device="cuda") < 1 - 30 / V
+    late = torch.arange(V, device="cuda").expand(rows, V) < V - 5
+    for x in (z.masked_fill(sparse, -INF), z.masked_fill(sparse, torch.finfo(t).min), z.masked_fill(late, -INF), torch.full_like(z, 0.5),
+              z.round(), z.clamp(max=0.0), torch.where(late, -0.0, 0.0), z.masked_fill(late, float("nan")).masked_fill(~late, 1.0)):
+        x = x.to(t)
+        for view in (x, ref.strided(x, 3, 1)):
+            _, _, _, _, ids = he.he_token_log_probs(ctx, view, y, top=top)
+            assert torch.equal(ids, ref.log_probs(x, y, top)[4])
+        if not torch.isnan(x).any():
+            check_log_probs(ctx, x, y, top)
+
+
 def test_log_probs_of_rows_that_are_not_finite(ctx):
     z, y = logits_of(5, 3000, "f32", 3, False)
     y[:] = 5
