@@ -98,6 +98,14 @@ def test_pieces_that_a_cluster_has_not_all(ctx, dtype, V):
         check_log_probs(ctx, ref.strided(z, 1, 1), y, 3)
 
 
+@pytest.mark.parametrize("dtype,rows,V,top", [("f16", 700, 860, 32), ("bf16", 500, 300, 64), ("bf16", 300, 1100, 33), ("f32", 900, 70, 64), ("f16", 40, 4100, 64),
+                                              ("bf16", 3, 33000, 64)])
+def test_rows_that_do_not_fill_a_piece(ctx, dtype, rows, V, top):
+    z, y = logits_of(rows, V, dtype, V + top, False)
+    check_log_probs(ctx, z, y, top)
+    check_log_probs(ctx, ref.strided(z, 1, 3), y, top)
+
+
 def test_many_rows(ctx):
     g = gen(3)
     rows = 150001
