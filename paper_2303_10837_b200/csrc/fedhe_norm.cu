@@ -375,7 +375,8 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
 }
 
 // A warp for each row, where there are rows enough: what threads do once for a row (sums over the warp, the row's numbers, the copies) is done by 32 of
-// them and not by the 256 of a group above, of which it was two thirds of all instructions.  32768 rows of 4096 in bf16: 98 us, 5.5 TB/s.  The weights are in shared memory, in packs of four, [weight, bias][fours of a pack][packs].
+// them and not by the 256 of a group above, of which it was two thirds of all instructions.  32768 rows of 4096 in bf16: 98 us, 5.5 TB/s.  The
+// weights are in shared memory, in packs of four, [weight, bias][fours of a pack][packs].
 template <class T, int HELD, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, 1) norm_warp_kernel(const NormArgs a, const RowPlan plan, int *status) {
     constexpr int V = WIDE<T>, K = HELD / V, FOURS = V / 4;
@@ -879,7 +880,8 @@ bool norm_grad_go(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, 
 }
 
 // Elements of a thread: 32 for long rows and, of 16-bit types, for much work, of which each row's own instructions then are a smaller part; 16 where what comes
-// before and behind the rows counts more, or memory (16384 rows of 4096 in bf16: 108 us with samples and 86 without, with 16 elements 139 and 109; 4096 rows of 1024:
+// before and behind the rows counts more, or memory (16384 rows of 4096 in bf16: 108 us with samples and 86 without, with 16 elements 139 and
+// 109; 4096 rows of 1024:
 // 31 and 22, 27 and 19; 16384 rows of 4096 in fp32: 164 and 151, 160 and 149).
 template <class T, int V>
 bool norm_grad_held(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {

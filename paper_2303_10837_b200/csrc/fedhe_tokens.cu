@@ -254,7 +254,8 @@ __device__ __noinline__ float bound_of_part(Found &f, const T *p, uint32_t count
     return value_of(bound + above);
 }
 
-// Fewer than `top` values were above the order f.edge (of many equal values, or -inf), which the first piece alone has so many values from on: the rest are of that order, and those with
+// Fewer than `top` values were above the order f.edge (of many equal values, or -inf), which the first piece alone has so many values from on:
+// the rest are of that order, and those with
 // the lowest indices lie in that piece.  By a warp; returns how many there are then.
 template <class T>
 __device__ __noinline__ uint32_t fill(Found &f, uint32_t now, uint32_t held, const T *p, uint32_t count, uint32_t first, uint32_t top) {
