@@ -180,7 +180,7 @@ __device__ __forceinline__ uint32_t highest_of_warp(uint32_t mine, uint32_t k) {
     return got;
 }
 // The order of the top-th value of what the block's threads hold, or a little less, given each thread's maximum: in each warp the (top / warps)-th highest
-// maximum of a thread, and the lowest of these over the warps.
+// maximum of a thread, and the lowest of these over the warps.  top is at most the number of threads: a warp has 32 maxima.
 __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32_t top) {
     const uint32_t warps = blockDim.x / 32, lane = threadIdx.x & 31u;
     const uint32_t got = highest_of_warp(mine, (top + warps - 1) / warps);
@@ -191,7 +191,8 @@ __device__ __forceinline__ uint32_t bound_of_top(Found &f, uint32_t mine, uint32
     if (threadIdx.x == 0) f.edge = low;
     return low;
 }
-// The same of a piece that the row does not fill, where some threads have little or nothing: in each warp the top-th highest maximum of a pack or a little less,
+// The same of a piece that the row does not fill, where some threads have little or nothing, or that has fewer threads than `top` (a row of 2 KB
+// that one warp holds whole, with more than 32 alternatives): in each warp the top-th highest maximum of a pack or a little less,
 // found by halving, and the highest of these; where packs are few, the top-th value itself (20000 rows of 300 in bf16 with 64 alternatives: 370 us, and 2330 from
 // the packs; 6297 of 860 in fp16 with eight: 55 and 66 from the values).  Returns what a candidate has at least: that, or the next above it where many
 // are equal to it.
@@ -388,7 +389,7 @@ __global__ void __launch_bounds__(256, 3) log_probs_kernel(const LogProbsArgs a,
         float from = -INFINITY;              // what a candidate has at least: that or the next above it, later the next above the top-th value so far
         uint32_t raise = 1;                  // the piece after which the bound is raised next
         bool lost = false;
-        const bool filled = (rank + 1) * NT * PACKS <= row.vectors;
+        const bool filled = (rank + 1) * NT * PACKS <= row.vectors && a.top <= NT;
         if (TOP && !filled && rank < pieces) from = bound_of_part<T>(f, row.p, n, (rank * NT + warp * 32) * PACKS + lane, row.vectors - rank * NT * PACKS, a.top);
         for (uint32_t c = rank; c < pieces; c += C, round++) {
             if (!gone && !copies_done(bar + d * 8, turn)) gone = true;
