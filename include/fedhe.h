@@ -397,7 +397,8 @@ int he_token_log_probs(he_ctx *ctx, const void *logits_dev, int dtype, size_t ro
  *   dlogits_j = sum_i g_i (d_{j,t_i} - p_j) - dentropy p_j (ln p_j + entropy)
  * over the target (g = dlogp; none for y < 0) and the alternatives (t =
  * top_ids, g = dtop, [rows][top]; top = 0: none).  dentropy may be NULL, and
- * entropy then too.  A row into which no gradient flows (no target, no
+ * entropy then too; |dentropy| up to 2^120 (beyond it a masked logit's may be
+ * NaN instead of 0).  A row into which no gradient flows (no target, no
  * dentropy, no dtop) or that holds nothing but -inf gives zeros whatever it
  * holds.  dlogits may be logits itself, with the same stride. */
 int he_token_log_probs_backward(he_ctx *ctx, const void *logits_dev, int dtype, size_t rows, size_t vocab, size_t row_stride,

@@ -17,7 +17,10 @@ namespace fedhe {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float FAR = -1e20f;             // exponents stop here: 2^FAR is 0, and FAR times what a row sums up to or a gradient is no infinity
+constexpr float FAR = -1e20f;             // exponents stop here: 2^FAR is 0, and FAR times what a row sums up to is no infinity
+// In the gradient ln p stops here, where p is 0 already: times an entropy's gradient of up to 2^120 it is no infinity, which 0 would make NaN (p times
+// the gradients first holds for all of them, and takes 193 us for 8192 x 32768 in bf16 with the entropy's where this takes 186).
+constexpr float LEAST_LN = -104.0f;
 constexpr int PACKS = 4;                  // of 16 bytes, that a thread has of a piece
 constexpr uint32_t PLACES = 256;          // for candidates of a warp
 constexpr uint32_t DEPTH = 3;             // pieces that a warp asks for ahead
@@ -710,8 +713,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, GRAD_BLOCKS) log_probs_grad_kern
                     const F2 l = two_of(z[i], e) + F2(-f.lse);
                     if (ENTROPY) {
                         float2 lp = l.both();
-                        lp.x = max_nan(lp.x, FAR);
-                        lp.y = max_nan(lp.y, FAR);
+                        lp.x = max_nan(lp.x, LEAST_LN);
+                        lp.y = max_nan(lp.y, LEAST_LN);
                         const float2 t = (F2(lp.x, lp.y) * F2(LOG2E)).both();
                         g[e] = F2(-ex2(t.x), -ex2(t.y)) * fma2(F2(f.gh), F2(lp.x, lp.y) + F2(f.H), F2(f.G));
                     } else {

@@ -41,3 +41,21 @@ def test_alternatives_of_rows_that_just_fill_a_piece(ctx, dtype, threads):
                     assert torch.equal(got, want[:, :top]), (V, shift, top)
             if V % per == per - 1:
                 check_log_probs(ctx, views[0], y, 64)
+
+
+@pytest.mark.parametrize("size", [1e17, 1e19, 1e30, 2.0 ** 117])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_gradients_of_the_entropy_and_masked_logits(ctx, dtype, size):
+    """p_j (ln p_j + H) is 0 where p_j is, whatever gradient it is multiplied by."""
+    z, y = logits_of(5, 3000, dtype, 19, True)
+    z[1:, 1::7] = torch.finfo(z.dtype).min
+    lse, entropy, ids = check_log_probs(ctx, z, y, 3)
+    g = gen(6)
+    dlogp, dent, dtop = randn(g, 5) * size, randn(g, 5) * size, randn(g, 5, 3) * size
+    hit = torch.zeros_like(z, dtype=torch.bool).scatter_(1, y.clamp(min=0)[:, None], True).scatter_(1, ids, True)
+    for top in ({}, {"top_ids": ids, "dtop": dtop}):
+        got = he.he_token_log_probs_backward(ctx, z, y, lse, dlogp, entropy=entropy, dentropy=dent, **top)
+        want, tol = ref.log_probs_grad(z, y, lse, dlogp, entropy, dent, top.get("top_ids"), top.get("dtop"))
+        # a p below 2^-126 may count as 0, and with it what it is multiplied by: at most 100 times 5 sizes, or 2^9
+        ref.close(got, want, tol + ref.rounding(want, z.dtype) + 2.0 ** -117 * size, "dlogits")
+        assert (got[(z < -1e30) & ~hit] == 0).all()
