@@ -395,8 +395,9 @@ int he_token_log_probs(he_ctx *ctx, const void *logits_dev, int dtype, size_t ro
                        float *top_logp_dev, int64_t *top_ids_dev, void *stream);
 /* Its gradient, from the lse (and entropy) that it gave:
  *   dlogits_j = sum_i g_i (d_{j,t_i} - p_j) - dentropy p_j (ln p_j + entropy)
- * over the target (g = dlogp; none for y < 0) and the alternatives (t =
- * top_ids, g = dtop, [rows][top]; top = 0: none).  dentropy may be NULL, and
+ * over the target (g = dlogp; none for y < 0, NaN for y >= vocab) and the
+ * alternatives (t = top_ids, g = dtop, [rows][top]; top = 0: none; of one outside
+ * [0, vocab) only -g p_j is left).  dentropy may be NULL, and
  * entropy then too; |dentropy| up to 2^120 (beyond it a masked logit's may be
  * NaN instead of 0).  A row into which no gradient flows (no target, no
  * dentropy, no dtop) or that holds nothing but -inf gives zeros whatever it

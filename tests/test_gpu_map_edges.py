@@ -59,3 +59,18 @@ def test_large_gradients_of_the_entropy_and_masked_logits(ctx, dtype, size):
         # a p below 2^-126 may count as 0, and with it what it is multiplied by: at most 100 times 5 sizes, or 2^9
         ref.close(got, want, tol + ref.rounding(want, z.dtype) + 2.0 ** -117 * size, "dlogits")
         assert (got[(z < -1e30) & ~hit] == 0).all()
+
+
+def test_alternatives_outside_the_vocabulary(ctx):
+    """Their gradients flow off the other logits, as the formula says, and reach none."""
+    z, y = logits_of(3, 700, "f32", 4, False)
+    y[:] = torch.tensor([3, -1, 699])
+    _, lse, _, _, ids = he.he_token_log_probs(ctx, z, y, top=4)
+    dlogp, dtop = randn(gen(1), 3), randn(gen(2), 3, 4)
+    ids[0, 1], ids[1, 2], ids[2, 3] = -1, 700, 2 ** 40
+    got = he.he_token_log_probs_backward(ctx, z, y, lse, dlogp, top_ids=ids, dtop=dtop)
+    # as many columns more as it takes, with p = 0
+    inside = torch.where((ids < 0) | (ids >= 700), torch.full_like(ids, 700), ids)
+    more = torch.cat([z, torch.full((3, 1), float("-inf"), device="cuda")], 1)
+    want, tol = ref.log_probs_grad(more, y, lse, dlogp, None, None, inside, dtop)
+    ref.close(got, want[:, :700], (tol + ref.rounding(want, z.dtype) + 2.0 ** -126)[:, :700], "dlogits")
