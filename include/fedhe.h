@@ -438,7 +438,9 @@ int he_layer_norm_backward(he_ctx *ctx, const void *dy_dev, size_t dy_stride, co
  * row of x and of dy begins on a 16-byte boundary (their strides are then at
  * least their widths).  HE_F32 operands, magnitudes of rows and rows at other
  * addresses are laid out there first.  fp32 products are taken from all 24 bits
- * of either factor. */
+ * of either factor, or of one below 2^-110 from what is above 2^-134; a factor of
+ * fp32 that is not finite makes the entries it meets NaN (an infinity of 16 bits
+ * makes them infinite, as the formula says). */
 size_t he_linear_sensitivity_work_bytes(const he_ctx *ctx, int dtype, size_t rows, size_t inputs, size_t outputs,
                                         int samples, int aligned);
 int he_linear_sensitivity(he_ctx *ctx, const void *x_dev, size_t x_stride, const void *dy_dev, size_t dy_stride, int dtype,

@@ -599,7 +599,8 @@ __global__ void __launch_bounds__(THREADS, 1) linear_map_kernel(const __grid_con
 // ---- operands that TMA cannot take as they are ----
 
 // The values v as the tensor cores take them: bf16 or fp16 as they are, fp32 as three bf16 pieces whose sum is v (each the rounding
-// of what the pieces before it leave; an infinity or a NaN is its own first piece).  Magnitudes where rows are samples of their own; those of dy
+// of what the pieces before it leave; below 2^-110 the last one ends at bf16's smallest step).  An infinity or a NaN is its own first piece: what it
+// meets becomes NaN, since an infinity is multiplied by the other factor's smaller pieces too, which are 0 or of either sign.  Magnitudes where rows are samples of their own; those of dy
 // are summed on the way, for the bias.
 struct StageArgs {
     MatArg in[2];            // x, dy

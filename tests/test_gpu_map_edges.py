@@ -74,3 +74,31 @@ def test_alternatives_outside_the_vocabulary(ctx):
     more = torch.cat([z, torch.full((3, 1), float("-inf"), device="cuda")], 1)
     want, tol = ref.log_probs_grad(more, y, lse, dlogp, None, None, inside, dtop)
     ref.close(got, want[:, :700], (tol + ref.rounding(want, z.dtype) + 2.0 ** -126)[:, :700], "dlogits")
+
+
+@pytest.mark.parametrize("alone", [False, True])
+def test_linear_map_of_infinities(ctx, alone):
+    """16-bit ones give infinite entries, those of fp32 entries that are not numbers; either in their own rows and columns alone."""
+    g = gen(8)
+    x, dy = torch.randint(1, 4, (50, 40), generator=g, device="cuda").float(), torch.randint(1, 4, (50, 24), generator=g, device="cuda").float()
+    x[7, 3] = float("inf")
+    dy[30, 5] = -float("inf")
+    cuts = None if alone else torch.tensor([0, 20, 45], dtype=torch.int32, device="cuda")
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        w, b = he.he_linear_sensitivity(ctx, x.to(dtype), dy.to(dtype), samples=cuts)
+        hit = torch.zeros_like(w, dtype=torch.bool)
+        hit[:, 3] = hit[5, :] = True
+        assert torch.isfinite(w[~hit]).all() and b[5] == float("inf") and torch.isfinite(b[:5]).all() and torch.isfinite(b[6:]).all()
+        assert (torch.isnan(w[hit]) if dtype == torch.float32 else torch.isinf(w[hit])).all()
+
+
+@pytest.mark.parametrize("exponent", [-109, -121, -129])
+def test_linear_map_of_the_smallest_values(ctx, exponent):
+    """Three pieces of bf16 hold a value of 2^-110 or more, and smaller ones to half of bf16's smallest step, 2^-134."""
+    g = gen(11)
+    dy = (torch.rand(64, 32, generator=g, device="cuda") + 1) * 2.0 ** -60 * 2.0 ** (exponent + 60)
+    x = (torch.rand(64, 48, generator=g, device="cuda") + 1) * 2.0 ** 60
+    for cuts in (None, [0, 20, 20, 64]):
+        got = he.he_linear_sensitivity(ctx, x, dy, samples=None if cuts is None else torch.tensor(cuts, dtype=torch.int32, device="cuda"))[0]
+        want, tol = ref.linear(x, dy, cuts)[0]
+        ref.close(got, want, tol + 2.0 ** -134 * x.double().sum(0), "map")
