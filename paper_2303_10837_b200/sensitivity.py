@@ -88,7 +88,9 @@ class _Linear(torch.autograd.Function):
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps, part, state):
-        rows = _rows(x)
+        rows, ctx.dtype = _rows(x), x.dtype
+        if torch.is_autocast_enabled(x.device.type):         # which computes and returns layer norms in fp32
+            rows, weight, bias = (None if t is None else t.float() for t in (rows, weight, bias))
         y, mean, rstd = he_layer_norm(state.ctx, rows, weight, bias, eps)
         ctx.save_for_backward(rows, weight, mean, rstd)
         ctx.part, ctx.state, ctx.shape = part, state, x.shape
@@ -106,7 +108,7 @@ class _LayerNorm(torch.autograd.Function):
             part.weight.add_(dweight)
         if part.bias is not None:
             part.bias.add_(dbias)
-        return dx.view(ctx.shape), None, None, None, None, None
+        return dx.view(ctx.shape).to(ctx.dtype), None, None, None, None, None
 
 
 def _parts(model: nn.Module, flat: torch.Tensor) -> List[Tuple[nn.Module, _Part]]:

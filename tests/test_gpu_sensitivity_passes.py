@@ -1,0 +1,67 @@
+"""A model's pass in sensitivity_map beside the model's own, and what it raises."""
+import pytest
+import torch
+from torch import nn
+
+import paper_2303_10837_b200 as he
+import synthetic_inputs as si
+from paper_2303_10837_b200.sensitivity import sensitivity_map
+from test_gpu_sensitivity import Model, batches, by_samples
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    return he.he_ctx_create(8192, list(si.PRIMES_N8192), 40)
+
+
+def test_layer_norms_under_autocast_are_those_of_torch(ctx):
+    """fp32 inside and out, whatever their inputs and weights are."""
+    torch.manual_seed(9)
+    data = batches(12, count=1)
+    for kind in (torch.float32, torch.bfloat16):
+        model = Model().cuda()
+        for m in model.modules():
+            if isinstance(m, nn.LayerNorm):
+                m.to(kind)
+        seen = []
+        hooks = [m.register_forward_hook(lambda m, args, out: seen.append(out.detach())) for m in model.modules() if isinstance(m, nn.LayerNorm)]
+        with torch.autocast("cuda", dtype=torch.bfloat16):
+            model(data[0][0])
+            there, seen[:] = list(seen), []
+            got = sensitivity_map(ctx, model, data)
+        for h in hooks:
+            h.remove()
+        assert len(there) == len(seen) == 5
+        for a, b in zip(there, seen):
+            # behind five layers at most, of which each may round a value of up to 4 the other way
+            assert a.dtype == b.dtype == torch.float32 and float((a - b).abs().max()) < 0.1
+        assert float((seen[0] - there[0]).abs().max()) < 1e-5
+        want = by_samples(model, data)
+        assert float((got.map - want).norm() / want.norm()) < 5e-2
+
+
+def test_a_layer_norm_behind_a_linear_layer_under_autocast(ctx):
+    """Its input is of autocast's type, its output is not."""
+    torch.manual_seed(10)
+    model = nn.Sequential(nn.Linear(20, 33), nn.LayerNorm(33), nn.Linear(33, 7)).cuda()
+    x, y = torch.randn(9, 4, 20, device="cuda"), torch.randint(0, 7, (9, 4), device="cuda")
+    seen = []
+    model[1].register_forward_hook(lambda m, args, out: seen.append((args[0].detach(), out.detach())))
+    for dtype in (torch.bfloat16, torch.float16):
+        seen.clear()
+        with torch.autocast("cuda", dtype=dtype):
+            model(x)
+            got = sensitivity_map(ctx, model, [(x, y)])
+        (a_in, a), (b_in, b) = seen
+        assert torch.equal(a_in, b_in) and a_in.dtype == dtype and a.dtype == b.dtype == torch.float32
+        assert float((a - b).abs().max()) < 1e-5             # of values up to 6: a few roundings of fp32
+        want = torch.zeros_like(got.map, dtype=torch.float64)
+        m = nn.Sequential(nn.Linear(20, 33), nn.LayerNorm(33), nn.Linear(33, 7)).cuda().double()
+        m.load_state_dict(model.state_dict())
+        for i in range(9):
+            m.zero_grad()
+            torch.log_softmax(m(x[i].double()), -1).gather(1, y[i][:, None]).sum().backward()
+            want += torch.cat([p.grad.reshape(-1).abs() for p in m.parameters()]) / 9
+        assert float((got.map - want).norm() / want.norm()) < 5e-2
