@@ -17,8 +17,8 @@ from typing import Dict, Iterable, List, NamedTuple, Optional, Tuple
 import torch
 from torch import nn
 
-from . import (HE_ERR_INVALID_ARG, Ctx, HeError, he_layer_norm, he_layer_norm_backward, he_linear_sensitivity, he_token_log_probs,
-               he_token_log_probs_backward)
+from . import (HE_ERR_INVALID_ARG, HE_OK, Ctx, HeError, he_ctx_status, he_layer_norm, he_layer_norm_backward, he_linear_sensitivity,
+               he_token_log_probs, he_token_log_probs_backward)
 
 
 class Sensitivity(NamedTuple):
@@ -180,7 +180,8 @@ def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Te
     layers too, and the model must not let one sample's activations depend on another's.  Scores are computed for the trained
     parameters of nn.Linear and nn.LayerNorm, each called once in a pass; a model that trains others, or uses these in another way, is
     refused.  Works under ``torch.autocast``.  No gradient is left behind, and the model's mode stays: with dropout, call
-    ``model.eval()`` first."""
+    ``model.eval()`` first.  Waits for the GPU at its end and reads the context's status, as he_ctx_status does: an error that the pass
+    or a call before it left there is raised, and the status cleared."""
     params = list(model.parameters())
     if not params or not params[0].is_cuda:
         raise TypeError("expected a model on a CUDA device")
@@ -213,4 +214,7 @@ def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Te
     if samples:
         flat /= samples
     log_prob, entropy, tokens = sums.tolist()
+    status = he_ctx_status(ctx)
+    if status != HE_OK:
+        raise HeError(status, "sensitivity_map: the context's status")
     return Sensitivity(flat, samples, int(tokens), log_prob / max(1, tokens), entropy / max(1, rows))

@@ -65,3 +65,19 @@ def test_a_layer_norm_behind_a_linear_layer_under_autocast(ctx):
             torch.log_softmax(m(x[i].double()), -1).gather(1, y[i][:, None]).sum().backward()
             want += torch.cat([p.grad.reshape(-1).abs() for p in m.parameters()]) / 9
         assert float((got.map - want).norm() / want.norm()) < 5e-2
+
+
+def test_an_error_inside_a_kernel_is_raised(ctx, monkeypatch):
+    from paper_2303_10837_b200 import sensitivity as sv
+    model, data = Model().cuda(), batches(2, count=1)
+    # one that is there: an encryption of what is not finite leaves it in the context
+    keys = he.he_keygen(ctx, 3)
+    he.he_encrypt(ctx, keys, he.he_pack(ctx, None, torch.full((8,), float("nan"), device="cuda"))[0], 1, 0)
+    with pytest.raises(he.HeError) as ei:
+        sensitivity_map(ctx, model, data)
+    assert ei.value.code == he.HE_ERR_OVERFLOW
+    sensitivity_map(ctx, model, data)                        # and it is no longer
+    monkeypatch.setattr(sv, "he_ctx_status", lambda c: he.HE_ERR_CUDA, raising=False)
+    with pytest.raises(he.HeError) as ei:
+        sensitivity_map(ctx, model, data)
+    assert ei.value.code == he.HE_ERR_CUDA
