@@ -12,6 +12,7 @@ he_encrypt take; the server's weighted sum of the clients' encrypted maps, decry
 from __future__ import annotations
 
 import contextlib
+import threading
 from typing import Dict, Iterable, List, NamedTuple, Optional, Tuple
 
 import torch
@@ -144,21 +145,38 @@ def _parts(model: nn.Module, flat: torch.Tensor) -> List[Tuple[nn.Module, _Part]
     return parts
 
 
+_taken: set = set()              # layers of the passes under way, by id
+_taking = threading.Lock()
+
+
 @contextlib.contextmanager
 def _layers_of(parts: List[Tuple[nn.Module, _Part]], state: _Pass):
-    """The trained layers go by the functions above while this lasts."""
+    """The trained layers go by the functions above while this lasts: in this thread, others' calls are refused."""
+    thread = threading.get_ident()
+
+    def enter(part, x):
+        if threading.get_ident() != thread:
+            _refuse("layer %s is called by another thread than the one whose pass it is in" % part.name)
+        state.enter(part, x.shape)
+
     def linear(m, part):
         def forward(x):
-            state.enter(part, x.shape)
+            enter(part, x)
             return _Linear.apply(x, m.weight, m.bias, part, state)
         return forward
 
     def norm(m, part):
         def forward(x):
-            state.enter(part, x.shape)
+            enter(part, x)
             return _LayerNorm.apply(x, m.weight, m.bias, m.eps, part, state)
         return forward
 
+    layers = {id(m) for m, _ in parts}
+    with _taking:
+        for m, part in parts:
+            if id(m) in _taken:
+                _refuse("layer %s is in a pass already" % part.name)
+        _taken.update(layers)
     before = [(m, m.__dict__.get("forward")) for m, _ in parts]
     try:
         for m, part in parts:
@@ -170,6 +188,8 @@ def _layers_of(parts: List[Tuple[nn.Module, _Part]], state: _Pass):
                 del m.forward
             else:
                 m.forward = own
+        with _taking:
+            _taken.difference_update(layers)
 
 
 def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Tensor, torch.Tensor]]) -> Sensitivity:
@@ -179,7 +199,8 @@ def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Te
     targets of the logits' leading shape; a negative target is none (padding).  Every entry of the first dimension is a sample, in the
     layers too, and the model must not let one sample's activations depend on another's.  Scores are computed for the trained
     parameters of nn.Linear and nn.LayerNorm, each called once in a pass; a model that trains others, or uses these in another way, is
-    refused.  Works under ``torch.autocast``.  No gradient is left behind, and the model's mode stays: with dropout, call
+    refused.  While a batch is passed through the model its trained layers' ``forward`` is replaced: calls by other threads are refused
+    meanwhile, and so is a second pass.  Works under ``torch.autocast``.  No gradient is left behind, and the model's mode stays: with dropout, call
     ``model.eval()`` first.  Waits for the GPU at its end and reads the context's status, as he_ctx_status does: an error that the pass
     or a call before it left there is raised, and the status cleared."""
     params = list(model.parameters())
