@@ -176,18 +176,16 @@ def _layers_of(parts: List[Tuple[nn.Module, _Part]], state: _Pass):
         for m, part in parts:
             if id(m) in _taken:
                 _refuse("layer %s is in a pass already" % part.name)
+            if "forward" in m.__dict__:
+                _refuse("layer %s has a forward of its own, which the pass would leave out" % part.name)
         _taken.update(layers)
-    before = [(m, m.__dict__.get("forward")) for m, _ in parts]
     try:
         for m, part in parts:
             m.forward = linear(m, part) if isinstance(m, nn.Linear) else norm(m, part)
         yield
     finally:
-        for m, own in before:
-            if own is None:
-                del m.forward
-            else:
-                m.forward = own
+        for m, _ in parts:
+            m.__dict__.pop("forward", None)
         with _taking:
             _taken.difference_update(layers)
 
@@ -198,8 +196,8 @@ def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Te
     ``batches``: pairs of inputs, which ``model`` turns into logits [samples][tokens][vocabulary] (or [samples][vocabulary]), and int64
     targets of the logits' leading shape; a negative target is none (padding).  Every entry of the first dimension is a sample, in the
     layers too, and the model must not let one sample's activations depend on another's.  Scores are computed for the trained
-    parameters of nn.Linear and nn.LayerNorm, each called once in a pass; a model that trains others, or uses these in another way, is
-    refused.  While a batch is passed through the model its trained layers' ``forward`` is replaced: calls by other threads are refused
+    parameters of nn.Linear and nn.LayerNorm, each called once in a pass; a model that trains others, or uses these in another way (by a
+    ``forward`` that was set on the module, for instance), is refused.  While a batch is passed through the model its trained layers' ``forward`` is replaced: calls by other threads are refused
     meanwhile, and so is a second pass.  Works under ``torch.autocast``.  No gradient is left behind, and the model's mode stays: with dropout, call
     ``model.eval()`` first.  Waits for the GPU at its end and reads the context's status, as he_ctx_status does: an error that the pass
     or a call before it left there is raised, and the status cleared."""

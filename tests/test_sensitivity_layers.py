@@ -56,3 +56,19 @@ def test_two_passes_at_once_are_refused_and_the_layers_come_back():
             assert torch.equal(model(x), want)
         assert all("forward" not in m.__dict__ for m in model)
     enter(places(model))
+
+
+def test_a_layer_with_a_forward_of_its_own_is_refused():
+    model = nn.Sequential(nn.Linear(4, 4), nn.Linear(4, 2))
+    plain = model[1].forward
+    model[1].forward = lambda x: plain(x) * 2
+
+    def enter():
+        with sv._layers_of(places(model), a_pass()):
+            pass
+
+    for _ in range(2):
+        refused(enter, "forward of its own")
+    assert "forward" in model[1].__dict__ and "forward" not in model[0].__dict__
+    del model[1].forward
+    enter()
