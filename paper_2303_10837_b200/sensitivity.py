@@ -58,6 +58,8 @@ class _Pass:
     def enter(self, part: _Part, shape: torch.Size) -> None:
         if len(shape) < 2 or shape[0] != self.count:
             _refuse("layer %s is given the shape %s: its first dimension has to be that of the %d samples" % (part.name, tuple(shape), self.count))
+        if not torch.is_grad_enabled():
+            _refuse("layer %s is run under no_grad, where it gets no score; give its parameters requires_grad=False if that is meant" % part.name)
         if part.name in self.seen:
             _refuse("layer %s is used twice in a pass: its two gradients would have to be added before their magnitudes are" % part.name)
         self.seen.add(part.name)
@@ -197,7 +199,8 @@ def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Te
     targets of the logits' leading shape; a negative target is none (padding).  Every entry of the first dimension is a sample, in the
     layers too, and the model must not let one sample's activations depend on another's.  Scores are computed for the trained
     parameters of nn.Linear and nn.LayerNorm, each called once in a pass; a model that trains others, or uses these in another way (by a
-    ``forward`` that was set on the module, for instance), is refused.  While a batch is passed through the model its trained layers' ``forward`` is replaced: calls by other threads are refused
+    ``forward`` that was set on the module or under ``no_grad``, for instance), is refused.  Parameters without a score (those that are not trained,
+    and those of layers that no gradient reaches) have 0, which he_select_mask takes last.  While a batch is passed through the model its trained layers' ``forward`` is replaced: calls by other threads are refused
     meanwhile, and so is a second pass.  Works under ``torch.autocast``.  No gradient is left behind, and the model's mode stays: with dropout, call
     ``model.eval()`` first.  Waits for the GPU at its end and reads the context's status, as he_ctx_status does: an error that the pass
     or a call before it left there is raised, and the status cleared."""

@@ -72,3 +72,22 @@ def test_a_layer_with_a_forward_of_its_own_is_refused():
     assert "forward" in model[1].__dict__ and "forward" not in model[0].__dict__
     del model[1].forward
     enter()
+
+
+def test_a_trained_layer_without_a_gradient_is_refused():
+    class Stops(nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.a, self.b = nn.Linear(4, 4), nn.Linear(4, 2)
+
+        def forward(self, x):
+            with torch.no_grad():
+                x = self.a(x)
+            return self.b(x)
+
+    model, x = Stops(), torch.randn(3, 4)
+    with sv._layers_of(places(model), a_pass()):
+        refused(lambda: model(x), "no_grad")
+    model.a.requires_grad_(False)
+    with sv._layers_of(places(model), a_pass()):
+        assert model(x).requires_grad
