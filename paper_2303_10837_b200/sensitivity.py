@@ -52,7 +52,9 @@ class _Pass:
     def samples(self, rows: int) -> Optional[torch.Tensor]:
         """Offsets of the batch's samples in a layer's rows (None: a row each)."""
         if rows not in self.offsets:
-            self.offsets[rows] = None if rows == self.count else torch.arange(0, rows + 1, rows // self.count, dtype=torch.int32, device=self.device)
+            self.offsets[rows] = None if rows == self.count else \
+                torch.arange(0, rows + 1, rows // self.count, dtype=torch.int32, device=self.device) if rows else \
+                torch.zeros(self.count + 1, dtype=torch.int32, device=self.device)
         return self.offsets[rows]
 
     def enter(self, part: _Part, shape: torch.Size) -> None:

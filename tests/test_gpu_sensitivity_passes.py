@@ -81,3 +81,20 @@ def test_an_error_inside_a_kernel_is_raised(ctx, monkeypatch):
     with pytest.raises(he.HeError) as ei:
         sensitivity_map(ctx, model, data)
     assert ei.value.code == he.HE_ERR_CUDA
+
+
+def test_a_layer_of_no_rows(ctx):
+    """A model with a part that a batch gives nothing to."""
+    class Parts(nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.a, self.n, self.b = nn.Linear(6, 6), nn.LayerNorm(6), nn.Linear(6, 5)
+
+        def forward(self, x):
+            return self.b(torch.cat([x, self.n(self.a(x[:, :0]))], 1))
+
+    torch.manual_seed(3)
+    model, x, y = Parts().cuda(), torch.randn(4, 3, 6, device="cuda"), torch.randint(0, 5, (4, 3), device="cuda")
+    got = sensitivity_map(ctx, model, [(x, y)]).map
+    head = nn.Sequential(model.b)
+    assert (got[:54] == 0).all() and torch.equal(got[54:], sensitivity_map(ctx, head, [(x, y)]).map)

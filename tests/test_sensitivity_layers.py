@@ -91,3 +91,9 @@ def test_a_trained_layer_without_a_gradient_is_refused():
     model.a.requires_grad_(False)
     with sv._layers_of(places(model), a_pass()):
         assert model(x).requires_grad
+
+
+def test_a_layer_of_no_rows():
+    state = a_pass()
+    state.enter(sv._Part("x", None, None), torch.Size((3, 0, 7)))
+    assert state.samples(0).tolist() == [0, 0, 0, 0] and state.samples(0).dtype == torch.int32
