@@ -5,8 +5,9 @@
 //   dx = rstd (a - mean(a) - n mean(a n)),  a = dy gamma
 //   dgamma = sum_t dy n,  dbeta = sum_t dy;   with samples  sum_k |sum_{t in k} dy n|,  sum_k |sum_{t in k} dy|
 //
-// All sums are in fp32.  Everything would be bounded by reading the inputs and writing the results once: 32768 rows of 4096 in bf16 take 95 us, 5.7
-// TB/s, the backward pass of 16384 rows 86; what is left is the sums over a row, for which its threads wait, and with few rows the beginning and the end.
+// All sums are in fp32.  Everything would be bounded by reading the inputs and writing the results once: 32768 rows of 4096 in bf16 take 94 us, 5.7
+// TB/s (98 by themselves), the backward pass of 16384 rows 88; what is left is the sums over a row, for which its threads wait, and with few rows the
+// beginning and the end.
 #include "fedhe_map.cuh"
 
 namespace fedhe {
@@ -140,8 +141,8 @@ struct RunsOut {
 // ---- a row at a time, held in registers ----
 
 // How a row is shared out: `threads` threads (a multiple of 32), each with `held` elements, `groups` of them in a block.  A group's rows come to
-// shared memory by bulk copies, `depth` rows ahead: that many loads in registers would leave room for few warps (rows one ahead in
-// registers: 176 us for 32768 rows of 4096 in bf16, by copies 114).
+// shared memory by bulk copies, `depth` rows ahead: that many loads in registers would leave room for few warps (32768 rows of 4096 in
+// bf16: one ahead in registers 176 us, by copies 119).
 struct RowPlan {
     uint32_t threads, groups, depth;
     uint32_t room;                                           // bytes of a row in shared memory
@@ -375,7 +376,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS) norm_kernel(const NormArgs a,
 }
 
 // A warp for each row, where there are rows enough: what threads do once for a row (sums over the warp, the row's numbers, the copies) is done by 32 of
-// them and not by the 256 of a group above, of which it was two thirds of all instructions.  32768 rows of 4096 in bf16: 98 us, 5.5 TB/s.  The
+// them and not by the 256 of a group above, of which it was two thirds of all instructions.  32768 rows of 4096 in bf16: 98 us where groups take 119.  The
 // weights are in shared memory, in packs of four, [weight, bias][fours of a pack][packs].
 template <class T, int HELD, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, 1) norm_warp_kernel(const NormArgs a, const RowPlan plan, int *status) {
@@ -825,8 +826,8 @@ bool norm_go(const NormArgs &a, int n_sm, int *status, cudaStream_t s, cudaError
     return true;
 }
 
-// With fewer than eight rows for each warp the groups below, which are more threads to a row, are as fast or faster (8192 rows of 4096 in fp32: 53 and 51 us,
-// 32768: 182 and 188; in bf16 35 and 37, 98 and 119; 32768 rows of 768 in bf16 27 and 35).
+// With fewer than eight rows for each warp the groups below, which are more threads to a row, are as fast or faster (calls by themselves: 8192 rows of 4096
+// in fp32 53 and 51 us, 32768: 182 and 188; in bf16 35 and 37, 98 and 119; 32768 rows of 768 in bf16 27 and 35).
 template <class T, int HELD, int WARPS>
 bool norm_warp_go(const NormArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
     if (a.width > 32 * HELD || a.rows < (size_t)8 * WARPS * n_sm) return false;
@@ -880,9 +881,8 @@ bool norm_grad_go(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, 
 }
 
 // Elements of a thread: 32 for long rows and, of 16-bit types, for much work, of which each row's own instructions then are a smaller part; 16 where what comes
-// before and behind the rows counts more, or memory (16384 rows of 4096 in bf16: 108 us with samples and 86 without, with 16 elements 139 and
-// 109; 4096 rows of 1024:
-// 31 and 22, 27 and 19; 16384 rows of 4096 in fp32: 164 and 151, 160 and 149).
+// before and behind the rows counts more, or memory (16384 rows of 4096 in bf16: 108 us with samples and 88 without, with 16 elements 139 and
+// 109; 4096 rows of 1024: 31 and 22, 27 and 19; 16384 rows of 4096 in fp32: 164 and 151, 160 and 149).
 template <class T, int V>
 bool norm_grad_held(const NormGradArgs &a, int n_sm, int *status, cudaStream_t s, cudaError_t &rc) {
     const bool many = V > 1 && sizeof(T) == 2 && a.width > 512 && a.rows * a.width >= (size_t)1 << 23;

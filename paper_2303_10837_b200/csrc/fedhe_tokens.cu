@@ -4,8 +4,10 @@
 //   dz_j = sum_i g_i (d_{j,t_i} - p_j) - g_H p_j (log p_j + H)        t_i: the target and the alternatives, g_i their gradients
 //
 // Both directions would be bounded by reading (and writing) the logits once.  The gradient is: 8192 x 32768 in bf16 take 170 us, 6.3 TB/s.  Log
-// probabilities of 2048 x 131072 in bf16 take 135 us with eight alternatives, 4.0 TB/s, and 111 without, which a quarter of the arithmetic does
-// not change: rows are read side by side, one for each block.
+// probabilities of 2048 x 131072 in bf16 take 135 us with eight alternatives, 4.0 TB/s, and 111 without.  888 blocks have a row each at a time: calls
+// by themselves without alternatives take 57 us for 888 rows, 70 for 900, 102 for 1776, 107 for 1790, 113 for 2048, 144 for 2664.  So the first rows cost
+// a call some 20 us more than their bytes, each new round of rows 4 to 12, and what comes in between runs at 6 to 7 TB/s; issue slots are 71 % used with
+// alternatives and without.
 #include <cooperative_groups.h>
 
 #include "fedhe_map.cuh"
@@ -758,7 +760,7 @@ template <class T>
 cudaError_t log_probs_grad_of(const LogProbsGradArgs &a, int n_sm, int *status, cudaStream_t s) {
     const uint32_t pieces = (uint32_t)((a.vocab * sizeof(T) + 15 + PIECE_BYTES - 1) / PIECE_BYTES), bytes = GRAD_THREADS / 32 * GRAD_DEPTH * PIECE_BYTES;
     // Parts of two pieces, so that warps that run side by side read and write side by side, and results that no cache holds past the caches
-    // (8192 x 32768 in bf16: parts of 16 pieces 219 us, of two 215; past the caches 211; with four blocks instead of six on an SM 166).
+    // (8192 x 32768 in bf16: parts of 16 pieces 219 us, of two 215; past the caches 211; with four blocks instead of six on an SM 170).
     const size_t most = (size_t)GRAD_BLOCKS * n_sm, warps = most * GRAD_THREADS / 32;
     const uint32_t run = a.rows * ((pieces + 1) / 2) < 4 * warps ? 1 : 2;
     const bool stream = a.rows * a.vocab * sizeof(T) > (size_t)64 << 20;
