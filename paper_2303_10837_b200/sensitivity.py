@@ -229,7 +229,9 @@ def sensitivity_map(ctx: Ctx, model: nn.Module, batches: Iterable[Tuple[torch.Te
             z, y = _rows(logits.detach()), targets.reshape(-1)
             logp, lse, entropy, _, _ = he_token_log_probs(ctx, z, y)
             dz = he_token_log_probs_backward(ctx, z, y, lse, torch.ones_like(lse))
-            if any(g is not None for g in torch.autograd.grad(logits, trained, dz.view(logits.shape), allow_unused=True)):
+            with torch.autocast(flat.device.type, enabled=False):        # each gradient is in the type of its part of the pass forward
+                grads = torch.autograd.grad(logits, trained, dz.view(logits.shape), allow_unused=True)
+            if any(g is not None for g in grads):
                 _refuse("a parameter is used other than by its layer's call")
         counted = y >= 0
         sums += torch.stack([torch.where(counted, logp, 0).sum(dtype=torch.float64), entropy.sum(dtype=torch.float64), counted.sum()])

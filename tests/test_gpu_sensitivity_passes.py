@@ -98,3 +98,22 @@ def test_a_layer_of_no_rows(ctx):
     got = sensitivity_map(ctx, model, [(x, y)]).map
     head = nn.Sequential(model.b)
     assert (got[:54] == 0).all() and torch.equal(got[54:], sensitivity_map(ctx, head, [(x, y)]).map)
+
+
+def test_parts_of_a_model_that_autocast_leaves_alone(ctx):
+    """Are differentiated in fp32 too: the pass backward is not under the caller's autocast."""
+    class Plain(nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.net = Model()
+
+        def forward(self, t):
+            with torch.autocast("cuda", enabled=False):
+                return self.net(t)
+
+    torch.manual_seed(11)
+    model, data = Plain().cuda(), batches(5)
+    want = sensitivity_map(ctx, model, data)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        got = sensitivity_map(ctx, model, data)
+    assert torch.equal(got.map, want.map) and got[1:] == want[1:]
