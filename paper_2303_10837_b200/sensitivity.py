@@ -18,7 +18,7 @@ from typing import Dict, Iterable, List, NamedTuple, Optional, Tuple
 import torch
 from torch import nn
 
-from . import (HE_ERR_INVALID_ARG, HE_OK, Ctx, HeError, he_ctx_status, he_layer_norm, he_layer_norm_backward, he_linear_sensitivity,
+from . import (HE_ERR_INVALID_ARG, HE_OK, Ctx, HeError, _stream, he_ctx_status, he_layer_norm, he_layer_norm_backward, he_linear_sensitivity,
                he_token_log_probs, he_token_log_probs_backward)
 
 
@@ -48,14 +48,28 @@ class _Pass:
         self.ctx, self.count, self.device = ctx, count, device
         self.offsets: Dict[int, Optional[torch.Tensor]] = {}
         self.seen: set = set()
+        self.home = torch.cuda.current_stream(device) if device.type == "cuda" else None
 
     def samples(self, rows: int) -> Optional[torch.Tensor]:
         """Offsets of the batch's samples in a layer's rows (None: a row each)."""
         if rows not in self.offsets:
-            self.offsets[rows] = None if rows == self.count else \
-                torch.arange(0, rows + 1, rows // self.count, dtype=torch.int32, device=self.device) if rows else \
-                torch.zeros(self.count + 1, dtype=torch.int32, device=self.device)
+            with torch.cuda.stream(self.home):
+                self.offsets[rows] = None if rows == self.count else \
+                    torch.arange(0, rows + 1, rows // self.count, dtype=torch.int32, device=self.device) if rows else \
+                    torch.zeros(self.count + 1, dtype=torch.int32, device=self.device)
         return self.offsets[rows]
+
+    @contextlib.contextmanager
+    def at_home(self):
+        """Work on the map, from the pass backward, which goes by the streams that the layers ran on: behind what the pass's own stream has
+        done to it (and to the samples' offsets), and ahead of what follows there."""
+        if _stream() == self.home.cuda_stream:
+            yield
+        else:
+            stream = torch.cuda.current_stream()
+            stream.wait_stream(self.home)
+            yield
+            self.home.wait_stream(stream)
 
     def enter(self, part: _Part, shape: torch.Size) -> None:
         if len(shape) < 2 or shape[0] != self.count:
@@ -85,8 +99,10 @@ class _Linear(torch.autograd.Function):
         x, weight = ctx.saved_tensors
         part, state = ctx.part, ctx.state
         rows = _rows(x)
-        he_linear_sensitivity(state.ctx, rows, _rows(dy), samples=state.samples(rows.shape[0]), out=part.weight, out_bias=part.bias, accumulate=True,
-                              bias=part.bias is not None)
+        samples = state.samples(rows.shape[0])
+        with state.at_home():
+            he_linear_sensitivity(state.ctx, rows, _rows(dy), samples=samples, out=part.weight, out_bias=part.bias, accumulate=True,
+                                  bias=part.bias is not None)
         return dy @ weight.to(dy.dtype) if ctx.needs_input_grad[0] else None, None, None, None, None
 
 
@@ -106,13 +122,14 @@ class _LayerNorm(torch.autograd.Function):
         rows, weight, mean, rstd = ctx.saved_tensors
         part, state = ctx.part, ctx.state
         every = state.samples(rows.shape[0])
-        if every is None:                                    # a row for each sample
-            every = torch.arange(rows.shape[0] + 1, dtype=torch.int32, device=rows.device)
-        dx, dweight, dbias = he_layer_norm_backward(state.ctx, _rows(dy), rows, mean, rstd, weight, samples=every)
-        if part.weight is not None:
-            part.weight.add_(dweight)
-        if part.bias is not None:
-            part.bias.add_(dbias)
+        with state.at_home():
+            if every is None:                                # a row for each sample
+                every = torch.arange(rows.shape[0] + 1, dtype=torch.int32, device=rows.device)
+            dx, dweight, dbias = he_layer_norm_backward(state.ctx, _rows(dy), rows, mean, rstd, weight, samples=every)
+            if part.weight is not None:
+                part.weight.add_(dweight)
+            if part.bias is not None:
+                part.bias.add_(dbias)
         return dx.view(ctx.shape).to(ctx.dtype), None, None, None, None, None
 
 

@@ -117,3 +117,37 @@ def test_parts_of_a_model_that_autocast_leaves_alone(ctx):
     with torch.autocast("cuda", dtype=torch.bfloat16):
         got = sensitivity_map(ctx, model, data)
     assert torch.equal(got.map, want.map) and got[1:] == want[1:]
+
+
+def test_layers_that_a_model_runs_on_another_stream(ctx):
+    """What they add to the map is there when it is divided, however late their stream comes to it."""
+    class Aside(nn.Module):
+        def __init__(self):
+            super().__init__()
+            self.a, self.n, self.b = nn.Linear(20, 33), nn.LayerNorm(33), nn.Linear(33, 7)
+            self.stream, self.wait = torch.cuda.Stream(), 0
+
+        def forward(self, x):
+            here = torch.cuda.current_stream()
+            self.stream.wait_stream(here)
+            with torch.cuda.stream(self.stream):
+                y = self.n(self.a(x))
+                if self.wait and y.requires_grad:
+                    y.register_hook(self.late)
+            here.wait_stream(self.stream)
+            return self.b(y)
+
+        def late(self, g):
+            torch.cuda._sleep(self.wait)                     # clocks
+            return g
+
+    torch.manual_seed(12)
+    model = Aside().cuda()
+    data = [(torch.randn(9, 4, 20, device="cuda"), torch.randint(0, 7, (9, 4), device="cuda")) for _ in range(3)]
+    plain = nn.Sequential(model.a, model.n, model.b)
+    want = sensitivity_map(ctx, plain, data)
+    for wait in (0, 20_000_000):
+        model.wait = wait
+        torch.cuda.synchronize()
+        got = sensitivity_map(ctx, model, data)
+        assert torch.equal(got.map, want.map) and got[1:] == want[1:]
