@@ -49,26 +49,29 @@ class _Pass:
         self.offsets: Dict[int, Optional[torch.Tensor]] = {}
         self.seen: set = set()
         self.home = torch.cuda.current_stream(device) if device.type == "cuda" else None
+        self.handle = self.home.cuda_stream if self.home else 0
 
     def samples(self, rows: int) -> Optional[torch.Tensor]:
         """Offsets of the batch's samples in a layer's rows (None: a row each)."""
         if rows not in self.offsets:
-            with torch.cuda.stream(self.home):
-                self.offsets[rows] = None if rows == self.count else \
-                    torch.arange(0, rows + 1, rows // self.count, dtype=torch.int32, device=self.device) if rows else \
-                    torch.zeros(self.count + 1, dtype=torch.int32, device=self.device)
+            self.offsets[rows] = None if rows == self.count else \
+                torch.arange(0, rows + 1, rows // self.count, dtype=torch.int32, device=self.device) if rows else \
+                torch.zeros(self.count + 1, dtype=torch.int32, device=self.device)
+            if self.home and self.offsets[rows] is not None:
+                self.offsets[rows].record_stream(self.home)      # other streams' uses are behind one another, and ahead of that one's
         return self.offsets[rows]
 
-    @contextlib.contextmanager
-    def at_home(self):
-        """Work on the map, from the pass backward, which goes by the streams that the layers ran on: behind what the pass's own stream has
-        done to it (and to the samples' offsets), and ahead of what follows there."""
-        if _stream() == self.home.cuda_stream:
-            yield
-        else:
-            stream = torch.cuda.current_stream()
-            stream.wait_stream(self.home)
-            yield
+    # The pass backward goes by the streams that the layers ran on.  Work on the map, and on the samples' offsets, comes there behind what the pass's own
+    # stream has to do, which goes on behind it.
+    def begin(self) -> Optional[torch.cuda.Stream]:
+        if _stream() == self.handle:
+            return None
+        stream = torch.cuda.current_stream()
+        stream.wait_stream(self.home)
+        return stream
+
+    def end(self, stream: Optional[torch.cuda.Stream]) -> None:
+        if stream is not None:
             self.home.wait_stream(stream)
 
     def enter(self, part: _Part, shape: torch.Size) -> None:
@@ -99,10 +102,10 @@ class _Linear(torch.autograd.Function):
         x, weight = ctx.saved_tensors
         part, state = ctx.part, ctx.state
         rows = _rows(x)
-        samples = state.samples(rows.shape[0])
-        with state.at_home():
-            he_linear_sensitivity(state.ctx, rows, _rows(dy), samples=samples, out=part.weight, out_bias=part.bias, accumulate=True,
-                                  bias=part.bias is not None)
+        stream = state.begin()
+        he_linear_sensitivity(state.ctx, rows, _rows(dy), samples=state.samples(rows.shape[0]), out=part.weight, out_bias=part.bias, accumulate=True,
+                              bias=part.bias is not None)
+        state.end(stream)
         return dy @ weight.to(dy.dtype) if ctx.needs_input_grad[0] else None, None, None, None, None
 
 
@@ -121,15 +124,16 @@ class _LayerNorm(torch.autograd.Function):
     def backward(ctx, dy):
         rows, weight, mean, rstd = ctx.saved_tensors
         part, state = ctx.part, ctx.state
+        stream = state.begin()
         every = state.samples(rows.shape[0])
-        with state.at_home():
-            if every is None:                                # a row for each sample
-                every = torch.arange(rows.shape[0] + 1, dtype=torch.int32, device=rows.device)
-            dx, dweight, dbias = he_layer_norm_backward(state.ctx, _rows(dy), rows, mean, rstd, weight, samples=every)
-            if part.weight is not None:
-                part.weight.add_(dweight)
-            if part.bias is not None:
-                part.bias.add_(dbias)
+        if every is None:                                    # a row for each sample
+            every = torch.arange(rows.shape[0] + 1, dtype=torch.int32, device=rows.device)
+        dx, dweight, dbias = he_layer_norm_backward(state.ctx, _rows(dy), rows, mean, rstd, weight, samples=every)
+        if part.weight is not None:
+            part.weight.add_(dweight)
+        if part.bias is not None:
+            part.bias.add_(dbias)
+        state.end(stream)
         return dx.view(ctx.shape).to(ctx.dtype), None, None, None, None, None
 
 
