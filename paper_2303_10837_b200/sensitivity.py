@@ -113,7 +113,8 @@ class _LayerNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps, part, state):
         rows, ctx.dtype = _rows(x), x.dtype
-        if torch.is_autocast_enabled(x.device.type):         # which computes and returns layer norms in fp32
+        # autocast computes and returns layer norms in fp32, those of 64 bits excepted
+        if torch.is_autocast_enabled(x.device.type) and x.dtype != torch.float64:
             rows, weight, bias = (None if t is None else t.float() for t in (rows, weight, bias))
         y, mean, rstd = he_layer_norm(state.ctx, rows, weight, bias, eps)
         ctx.save_for_backward(rows, weight, mean, rstd)

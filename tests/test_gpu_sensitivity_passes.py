@@ -151,3 +151,12 @@ def test_layers_that_a_model_runs_on_another_stream(ctx):
         torch.cuda.synchronize()
         got = sensitivity_map(ctx, model, data)
         assert torch.equal(got.map, want.map) and got[1:] == want[1:]
+
+
+def test_64_bits_are_refused_under_autocast_too(ctx):
+    model = nn.Sequential(nn.LayerNorm(6), nn.Linear(6, 5)).cuda().double()
+    x, y = torch.randn(4, 3, 6, device="cuda", dtype=torch.float64), torch.randint(0, 5, (4, 3), device="cuda")
+    for enabled in (False, True):
+        with torch.autocast("cuda", dtype=torch.bfloat16, enabled=enabled), pytest.raises(he.HeError) as ei:
+            sensitivity_map(ctx, model, [(x, y)])
+        assert ei.value.code == he.HE_ERR_INVALID_ARG and "float64" in str(ei.value)
